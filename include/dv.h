@@ -16,14 +16,17 @@
  *     (Section 4.3): dv_sparse_block, and dv_sparse_block_noalloc for callers
  *     that cannot allocate a workspace;
  *   - several layers of one token with the cross-layer look-ahead of Section 4.3:
- *     dv_sparse_decode.
+ *     dv_sparse_decode;
+ *   - a key/value cache in pages for serving programs and models with rotary positions:
+ *     dv_rope, dv_paged_append, dv_paged_attn (with a prefix that the batch shares
+ *     attended once), and the sparsified attention on such a cache, dv_sparse_attn_paged.
  * Aids: dv_set_launch_events / dv_launch_label (per-launch timing) and
  * dv_stream_read (a plain streaming read, the measured bandwidth ceiling).
  *
  * Conventions shared by every entry point
  *   Memory.   Every array pointer is a DEVICE pointer owned by the caller, except
  *             dv_kv.pos, which is a HOST array (the attention grid is sized from
- *             it on the host). The library never allocates or frees memory on
+ *             it on the host), and the output of dv_rotary_freqs. The library never allocates or frees memory on
  *             these paths and keeps no per-call state; scratch space is the
  *             caller's workspace `ws` of at least the size returned by the
  *             matching *_workspace_bytes query (256-byte aligned). Calls that
@@ -356,6 +359,129 @@ dv_status dv_sparse_block_noalloc(const dv_attn *a, const dv_mlp *m, const dv_pr
                                   const float *x_in, float *x_out, int32_t B, int32_t k_heads,
                                   int32_t k_mlp, int32_t mode, int32_t batch_mode, float scale,
                                   int32_t *heads_out, int32_t *idx_out, uint32_t flags, void *stream);
+
+/* ------------------------------------------------------------- rotary positions
+ * A vector of dh elements at position p is rotated pair by pair: pair i < rot/2 by the angle
+ * a = p freq[i],
+ *   (x0, x1) -> mscale (x0 cos a - x1 sin a, x0 sin a + x1 cos a);
+ * elements from rot on stay as they are. The angle is taken in 64 bits and reduced to one turn
+ * before its sine and cosine, so positions past 2^24 lose nothing.
+ *   layout  DV_ROPE_HALF: pair i is (i, i + rot/2); DV_ROPE_INTERLEAVED: (2i, 2i + 1).
+ *   freq    [rot/2] DEVICE doubles, 8-byte aligned: radians per position (dv_rotary_freqs).
+ *   mscale  factor on the rotated elements: 1, or what a rule for long contexts asks for.
+ * dv_rotary_freqs writes rot/2 frequencies to the HOST array freq, f_i = base^(-2i/rot), then
+ *   DV_ROPE_LINEAR  f_i / factor (positions interpolated; Chen et al., arXiv 2306.15595);
+ *   DV_ROPE_NTK     base replaced by base factor^(rot/(rot-2)): the last pair is interpolated, the
+ *                   first stays (needs rot > 2);
+ *   DV_ROPE_PARTS   with r = orig_len f_i / 2 pi turns in the original context and
+ *                   g = clamp((r - low) / (high - low), 0, 1): f_i (g + (1 - g) / factor)
+ *                   (Peng et al., arXiv 2309.00071, whose mscale is 0.1 ln(factor) + 1). */
+enum { DV_ROPE_HALF = 0, DV_ROPE_INTERLEAVED = 1 };
+enum { DV_ROPE_PLAIN = 0, DV_ROPE_LINEAR = 1, DV_ROPE_NTK = 2, DV_ROPE_PARTS = 3 };
+/* Flag of dv_rope alone: rotate by -a (times mscale): the transpose, so the gradient with
+ * respect to x is this of the gradient with respect to the output. */
+enum { DV_ROPE_INVERSE = 1u << 2 };
+typedef struct dv_rotary {
+  int32_t rot;          /* rotated elements, even, 2 <= rot <= dh */
+  int32_t layout;       /* DV_ROPE_HALF or DV_ROPE_INTERLEAVED */
+  const double *freq;   /* [rot/2], device */
+  float mscale;
+  int32_t reserved;     /* must be 0 */
+} dv_rotary;
+dv_status dv_rotary_freqs(int32_t rule, int32_t rot, double base, double factor, double orig_len, double low,
+                          double high, double *freq);
+
+/* dv_rope: out[t][h] = x[t][h] rotated at position pos[t], for T tokens of H heads of dh elements.
+ *   x, out  token t at x + t ldx (out + t ldo) elements, its heads contiguous; ld >= H dh; xtype
+ *           (DV_F16 or DV_F32) for both; fp32 inside, rounded to nearest even once. out == x with
+ *           ldo == ldx rotates in place. Pointers and strides need only the type's own alignment
+ *           (16-byte aligned rows take the wide path).
+ *   pos     [T] int32 device, any value (a negative one turns backwards).
+ * Limits: dh <= 256. T == 0 or H == 0 does nothing. */
+dv_status dv_rope(const dv_rotary *r, const void *x, int64_t ldx, int32_t xtype, int32_t T, int32_t H, int32_t dh,
+                  const int32_t *pos, void *out, int64_t ldo, uint32_t flags, void *stream);
+
+/* ------------------------------------------------------- key/value cache in pages
+ * The rows (positions) of a sequence lie in pages of `page` rows; row p of sequence s is row
+ * p % page of page table[s][p / page]. Of K and V alike, row r of head h in page g starts at
+ *   K + g page_stride + h head_stride + r row_stride   (elements),
+ * its dh elements contiguous: head-major or row-major pages, keys and values or several layers in
+ * one allocation. Strides are multiples of 16 bytes under which no two rows overlap.
+ * One table serves every layer of a model. A page may be in several sequences' rows (a shared
+ * prefix); whoever appends must hold the written page alone. */
+typedef struct dv_paged_kv {
+  int32_t H, dh;              /* key/value heads, head width (dh elements a multiple of 16 bytes, dh <= 256) */
+  int32_t page;               /* rows of a page (>= 1; any number) */
+  int32_t n_pages;            /* pages of the pool */
+  int32_t n_seq, max_pages;   /* the table's rows and their length; max_pages * page < 2^31 */
+  int32_t ktype;              /* dv_dtype of K and V: DV_F16 or DV_F32 */
+  int32_t reserved;           /* must be 0 */
+  int64_t page_stride, head_stride, row_stride;
+  void *K, *V;                /* device */
+  const int32_t *table;       /* [n_seq][max_pages] int32 DEVICE, page indices */
+} dv_paged_kv;
+
+/* dv_paged_append: keys and values of T new tokens into the cache, and their queries rotated.
+ * Token t belongs to row pos[t] of sequence seq[t]: K gets k[t][h] rotated there (r == NULL: as it
+ * is), V gets v[t][h], both rounded to nearest even to ktype.
+ *   k, v      [T][H][dh] of xtype at token strides ldk, ldv (as x of dv_rope).
+ *   seq, pos  [T] int32 device; seq NULL: token t is of sequence t. A token with pos < 0 (an idle
+ *             slot of the batch, padding) is left out: its queries are not rotated either. A
+ *             token whose sequence, row or page is out of range writes no key or value.
+ *   heads     NULL: every head; else [T][n_heads] int32 device: only those key/value heads are
+ *             written (Section 4.2), the others' rows are left untouched.
+ *   q, q_out  optional [T][Hq][dh] of xtype at ldq, ldqo: q_out = q rotated (q_out == q with equal
+ *             strides: in place). Without r they are copied.
+ * No two tokens may name the same row of the same sequence. T == 0 does nothing. */
+dv_status dv_paged_append(const dv_paged_kv *kv, const dv_rotary *r, const void *k, int64_t ldk, const void *v,
+                          int64_t ldv, int32_t xtype, int32_t T, const int32_t *seq, const int32_t *pos,
+                          const int32_t *heads, int32_t n_heads, const void *q, int64_t ldq, int32_t Hq, void *q_out,
+                          int64_t ldqo, void *stream);
+
+/* dv_paged_attn: decode attention of T query tokens over the cache (already appended to).
+ * Query head i reads key/value head i / (Hq / H); token t attends rows 0..pos[t] of its sequence:
+ *   out[t][j] = sum_p softmax_p(scale q[t][j] . K_p) V_p,  lse[t][j] = log sum_p exp(scale q . K_p).
+ * A token with pos < 0 attends nothing: out 0, lse -infinity. Several tokens of one sequence
+ * (drafts) each have their own pos; nothing beyond pos[t] influences token t, whatever lies there.
+ *   q         [T][n][dh] fp32 device, 16-byte aligned, n = n_heads with head sets, else Hq.
+ *   heads     NULL: all Hq heads; else [T][n_heads] int32 device: token t's head set (as dv_sparse_attn).
+ *   seq, pos  as for dv_paged_append.
+ *   max_len   host bound of the attended rows, 1 <= max_len <= max_pages * page: rows from max_len on
+ *             are not attended. It sizes the launch; a captured step keeps one that covers its replays.
+ *   shared_pages  the first shared_pages entries of the table rows of all tokens that attend at
+ *             least shared_pages * page rows are the same pages: those rows are read and computed once for
+ *             the batch. 0: none. (A token that attends fewer rows, an idle one among them, is
+ *             computed by itself.) shared_pages * page <= max_len.
+ *   out, lse  [T][n][dh] and [T][n] fp32 (lse may be NULL).
+ * Arithmetic to fp32's precision: fp16 products are exact on the matrix cores with queries and
+ * probabilities as sums of two halves (each within 2^-22 of its value; parts of a query below
+ * 2^-39 of its largest element vanish). An infinite or NaN key or value in an attended row makes
+ * the outputs of the heads that attend it NaN or infinite; others are not affected.
+ * A page index out of range is clamped (no fault, unspecified result); DV_VALIDATE checks on the
+ * device first that the attended rows' pages, the sequences and head sets are in range, that
+ * pos < max_len and that the shared pages are the same, and returns DV_ERR_INDEX otherwise.
+ * Limits: T * n <= 2^22, T * H <= 2^22. T == 0 does nothing. */
+size_t dv_paged_attn_workspace_bytes(const dv_paged_kv *kv, int32_t T, int32_t Hq, int32_t n_heads, int32_t max_len,
+                                     int32_t shared_pages);
+dv_status dv_paged_attn(const dv_paged_kv *kv, const float *q, int32_t T, int32_t Hq, const int32_t *heads,
+                        int32_t n_heads, const int32_t *seq, const int32_t *pos, int32_t max_len,
+                        int32_t shared_pages, float scale, float *out, float *lse, void *ws, size_t ws_bytes,
+                        uint32_t flags, void *stream);
+
+/* dv_sparse_attn_paged: dv_sparse_attn on a cache in pages, with rotary positions (r == NULL:
+ * without): out[b] = bo + sum_{i in S_A^b} H_i(x[b]) W^O_i, for B tokens (kv->H = a->H, kv->dh =
+ * a->dh). The fresh keys (rotated at pos[b]) and values of the selected heads are written to row
+ * pos[b] of sequence seq[b], then head i attends rows 0..pos[b]. A slot with pos[b] < 0 is idle:
+ * nothing is written and out[b] = bo. Tokens of one sequence in one call (drafts) are all
+ * appended before any attends.
+ *   heads, n_heads, scale, x, out as for dv_sparse_attn; seq, pos, max_len, shared_pages as for
+ *   dv_paged_attn. Limits as dv_sparse_attn (B > 1: B <= 32, fp16 weights). */
+size_t dv_sparse_attn_paged_workspace_bytes(const dv_attn *a, const dv_paged_kv *kv, int32_t B, int32_t n_heads,
+                                            int32_t max_len, int32_t shared_pages);
+dv_status dv_sparse_attn_paged(const dv_attn *a, const float *x, int32_t B, const dv_paged_kv *kv, const dv_rotary *r,
+                               const int32_t *seq, const int32_t *pos, int32_t max_len, int32_t shared_pages,
+                               const int32_t *heads, int32_t n_heads, float scale, float *out, void *ws,
+                               size_t ws_bytes, uint32_t flags, void *stream);
 
 #ifdef __cplusplus
 }

@@ -6,13 +6,13 @@ library is loaded from this package directory and nothing else is tried: if it i
 missing, loading raises (there is no CPU fallback).
 
 Entry points keep the C names: dv_predict_mlp, dv_predict_heads, dv_sparse_mlp,
-dv_sparse_attn, dv_sparse_block. Each takes the tensors, allocates outputs and the
+dv_sparse_attn, dv_sparse_block, dv_rope, dv_paged_append, dv_paged_attn and so on. Each takes the tensors, allocates outputs and the
 workspace with torch when they are not given, calls the C function on the current
 stream and raises DvError on a non-zero status.
 """
 import ctypes
 import os
-from ctypes import POINTER, c_char_p, c_float, c_int32, c_size_t, c_uint32, c_void_p
+from ctypes import POINTER, c_char_p, c_double, c_float, c_int32, c_int64, c_size_t, c_uint32, c_void_p
 from dataclasses import dataclass
 from typing import Optional
 
@@ -25,7 +25,9 @@ DV_ACT_RELU, DV_ACT_GELU = 0, 1
 DV_SELECT_TOPK, DV_SELECT_THRESHOLD = 0, 1
 DV_LOOKAHEAD, DV_SEQUENTIAL = 0, 1
 DV_MLP_UNION, DV_MLP_MASKED = 0, 1
-DV_DETERMINISTIC, DV_VALIDATE = 1, 2
+DV_DETERMINISTIC, DV_VALIDATE, DV_ROPE_INVERSE = 1, 2, 4
+DV_ROPE_HALF, DV_ROPE_INTERLEAVED = 0, 1
+DV_ROPE_PLAIN, DV_ROPE_LINEAR, DV_ROPE_NTK, DV_ROPE_PARTS = 0, 1, 2, 3
 (DV_OK, DV_ERR_NULL, DV_ERR_SHAPE, DV_ERR_DTYPE, DV_ERR_ALIGN, DV_ERR_WORKSPACE, DV_ERR_INDEX, DV_ERR_HIP,
  DV_ERR_UNSUPPORTED, DV_ERR_ARG) = range(10)
 
@@ -78,6 +80,17 @@ class CLayer(ctypes.Structure):
     _fields_ = [("attn", CAttn), ("mlp", CMlp), ("pa", CPredictor), ("pm", CPredictor), ("ln", CLN), ("kv", CKV)]
 
 
+class CRotary(ctypes.Structure):
+    _fields_ = [("rot", c_int32), ("layout", c_int32), ("freq", c_void_p), ("mscale", c_float), ("reserved", c_int32)]
+
+
+class CPagedKV(ctypes.Structure):
+    _fields_ = [("H", c_int32), ("dh", c_int32), ("page", c_int32), ("n_pages", c_int32), ("n_seq", c_int32),
+                ("max_pages", c_int32), ("ktype", c_int32), ("reserved", c_int32), ("page_stride", c_int64),
+                ("head_stride", c_int64), ("row_stride", c_int64), ("K", c_void_p), ("V", c_void_p),
+                ("table", c_void_p)]
+
+
 _PRED_ARGS = [POINTER(CPredictor), c_void_p, c_int32, c_int32, c_int32, c_float, c_void_p, c_int32,
               c_void_p, c_void_p, c_void_p, c_size_t, c_uint32, c_void_p]
 _SIGS = {
@@ -114,6 +127,21 @@ _SIGS = {
                                   POINTER(CLN), POINTER(CKV), c_void_p, c_void_p, c_int32, c_int32, c_int32,
                                   c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_size_t,
                                   c_uint32, c_void_p]),
+    "dv_rotary_freqs": (c_int32, [c_int32, c_int32, c_double, c_double, c_double, c_double, c_double,
+                                  POINTER(c_double)]),
+    "dv_rope": (c_int32, [POINTER(CRotary), c_void_p, c_int64, c_int32, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                          c_int64, c_uint32, c_void_p]),
+    "dv_paged_append": (c_int32, [POINTER(CPagedKV), POINTER(CRotary), c_void_p, c_int64, c_void_p, c_int64, c_int32,
+                                  c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_void_p, c_int64, c_int32, c_void_p,
+                                  c_int64, c_void_p]),
+    "dv_paged_attn_workspace_bytes": (c_size_t, [POINTER(CPagedKV), c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "dv_paged_attn": (c_int32, [POINTER(CPagedKV), c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p,
+                                c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_size_t, c_uint32, c_void_p]),
+    "dv_sparse_attn_paged_workspace_bytes": (c_size_t, [POINTER(CAttn), POINTER(CPagedKV), c_int32, c_int32, c_int32,
+                                                        c_int32]),
+    "dv_sparse_attn_paged": (c_int32, [POINTER(CAttn), c_void_p, c_int32, POINTER(CPagedKV), POINTER(CRotary), c_void_p,
+                                       c_void_p, c_int32, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p,
+                                       c_size_t, c_uint32, c_void_p]),
 }
 
 _lib = None
@@ -391,6 +419,59 @@ class LN:
         return self._cs
 
 
+@dataclass
+class Rotary:
+    """Rotary positions: freq [rot/2] float64 on the GPU (radians per position of each pair,
+    see rotary_freqs), the pairs' layout and the factor on the rotated elements."""
+    freq: torch.Tensor
+    layout: int = DV_ROPE_HALF
+    mscale: float = 1.0
+
+    def c(self) -> CRotary:
+        key = (id(self.freq), self.layout, self.mscale)
+        if getattr(self, "_ck", None) != key:
+            _tensor("Rotary.freq", self.freq, (torch.float64,), 1)
+            self._cs = CRotary(2 * self.freq.shape[0], int(self.layout), _ptr(self.freq), float(self.mscale), 0)
+            self._ck, self._kept = key, self.freq     # (kept: no other tensor gets its id)
+        return self._cs
+
+
+class PagedKV:
+    """A key/value cache in pages: K, V [n_pages][H][page][dh] (views of any strides with contiguous
+    rows, the same for both: K = pool[:, 0] and V = pool[:, 1] of one allocation, or
+    pool.transpose(1, 2) of pages that hold [page][H][dh]) and the block table [n_seq][max_pages] int32."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
+        self.K, self.V, self.table = K, V, table
+
+    def c(self) -> CPagedKV:
+        # checked and built once per set of tensors (calls are on the hot path)
+        key = (id(self.K), id(self.V), id(self.table))
+        if getattr(self, "_ck", None) != key:
+            for nm in ("K", "V"):
+                t = getattr(self, nm)
+                if not isinstance(t, torch.Tensor):
+                    raise TypeError(f"PagedKV.{nm} must be a torch.Tensor, not {type(t).__name__}")
+                if t.dtype not in _STORE:
+                    raise TypeError(f"PagedKV.{nm} has dtype {t.dtype}; expected {' or '.join(map(str, _STORE))}")
+                if t.dim() != 4:
+                    raise ValueError(f"PagedKV.{nm} must be 4-D, got shape {tuple(t.shape)}")
+                if t.shape[3] > 1 and t.stride(3) != 1:
+                    raise ValueError(f"PagedKV.{nm}: the elements of a row must be contiguous")
+            _same_dtype("PagedKV", self.K, self.V)
+            n_pages, H, page, dh = self.K.shape
+            strides = [s if n > 1 else dh for s, n in zip(self.K.stride()[:3], self.K.shape)]
+            if self.V.shape != self.K.shape or strides != [s if n > 1 else dh for s, n in
+                                                           zip(self.V.stride()[:3], self.V.shape)]:
+                raise ValueError("PagedKV: K and V must have the same shape and strides")
+            _tensor("PagedKV.table", self.table, _I32, 2, dev=False)
+            _gpu("PagedKV", self.K, self.V, self.table)
+            self._cs = CPagedKV(H, dh, page, n_pages, self.table.shape[0], self.table.shape[1], _wtype(self.K), 0,
+                                *strides, _ptr(self.K), _ptr(self.V), _ptr(self.table))
+            self._ck, self._kept = key, (self.K, self.V, self.table)   # (kept: no other tensor gets their ids)
+        return self._cs
+
+
 # ------------------------------------------------------------- entry points
 def _predict(fn, pred: Predictor, x, k=0, mode=DV_SELECT_TOPK, thresh=0.0, idx=None, count=None,
              scores=None, cap_idx=None, ws=None, flags=0, stream=None):
@@ -610,6 +691,200 @@ def dv_sparse_decode(layers, x, k_heads, k_mlp, scale, out=None, heads_out=None,
                               *_wsarg(ws), flags, _stream(stream))
     _check("dv_sparse_decode", st)
     return out, heads_out, idx_out
+
+
+# ------------------------------------------------- rotary positions, cache in pages
+def rotary_freqs(rot, base=10000.0, rule=DV_ROPE_PLAIN, factor=1.0, orig_len=0.0, low=1.0, high=32.0):
+    """The rot/2 frequencies (radians per position) as a float64 CPU tensor: base^(-2i/rot) as it is, with
+    positions interpolated (DV_ROPE_LINEAR), a larger base (DV_ROPE_NTK) or by parts (DV_ROPE_PARTS)."""
+    out = torch.empty(max(rot // 2, 1), dtype=torch.float64)
+    _check("dv_rotary_freqs", load().dv_rotary_freqs(rule, rot, base, factor, orig_len, low, high,
+                                                     ctypes.cast(out.data_ptr(), POINTER(c_double))))
+    return out
+
+
+def _here(*ts):
+    """Every tensor on the current device: the launch goes there, and elsewhere its pointers fault."""
+    dev = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{dev}")
+
+
+def _used_on(stream, *ts):
+    """Tensors that the binding allocated and a given stream uses: the allocator waits for it before reuse."""
+    if stream is not None:
+        s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+        for t in ts:
+            t.record_stream(s)
+
+
+def _tokens(name, x, heads=None, dh=None, rows=None, dtype=None):
+    """A [tokens][heads][dh] input of a storage type whose tokens may lie at any stride, each contiguous;
+    returns the stride."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, not {type(x).__name__}")
+    if x.dtype not in (_STORE if dtype is None else (dtype,)):
+        raise TypeError(f"{name} has dtype {x.dtype}; expected {dtype or ' or '.join(map(str, _STORE))}")
+    if x.dim() != 3 or any(w is not None and w != g for w, g in zip((rows, heads, dh), x.shape)):
+        raise ValueError(f"{name} has shape {tuple(x.shape)}; expected [tokens{'' if rows is None else f' = {rows}'}]"
+                         f"[heads{'' if heads is None else f' = {heads}'}][dh{'' if dh is None else f' = {dh}'}]")
+    if x.numel() and ((x.shape[2] > 1 and x.stride(2) != 1) or (x.shape[1] > 1 and x.stride(1) != x.shape[2])):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    if x.shape[0] > 1 and x.stride(0) < x.shape[1] * x.shape[2]:
+        raise ValueError(f"{name}: tokens overlap (stride {x.stride(0)})")
+    _gpu(name, x)
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+def _fits_i32(t, shape) -> bool:
+    return type(t) is torch.Tensor and t.dtype is torch.int32 and t.shape == shape and t.is_cuda and t.is_contiguous()
+
+
+def _index(name, t, shape, optional=False):
+    if not ((t is None and optional) or _fits_i32(t, shape)):
+        _tensor(name, t, _I32, len(shape), shape, optional=optional)
+
+
+def dv_rope(rotary: Rotary, x, pos, inverse=False, out=None, stream=None):
+    """x [T][H][dh] (fp16 or fp32) rotated at positions pos [T]; inverse: by the negative angles (the
+    gradient's direction). out=x rotates in place."""
+    lib = load()
+    cr = rotary.c()
+    ldx = _tokens("x", x)
+    T, H, dh = x.shape
+    _index("pos", pos, (T,))
+    mine = out is None
+    if mine:
+        out = torch.empty((T, H, dh), dtype=x.dtype, device=x.device)
+    ldo = ldx if out is x else _tokens("out", out, H, dh, T, x.dtype)
+    _here(x, pos, out, rotary.freq)
+    _check("dv_rope", lib.dv_rope(ctypes.byref(cr), _ptr(x), ldx, _wtype(x), T, H, dh, _ptr(pos), _ptr(out), ldo,
+                                  DV_ROPE_INVERSE if inverse else 0, _stream(stream)))
+    if mine:
+        _used_on(stream, out)
+    return out
+
+
+def dv_paged_append(kv: PagedKV, k, v, pos, seq=None, rotary: Optional[Rotary] = None, heads=None, q=None, q_out=None,
+                    stream=None):
+    """Keys and values k, v [T][H][dh] of new tokens into their rows pos [T] of sequences seq [T] (None: token t is
+    of sequence t), keys rotated if `rotary` is given; tokens with pos < 0 are left out. heads [T][n]: only
+    those key/value heads. q [T][Hq][dh]: rotated into q_out (q_out=q: in place), which is returned."""
+    lib = load()
+    ck = kv.c()
+    cr = rotary.c() if rotary is not None else None
+    ldk = _tokens("k", k, ck.H, ck.dh)
+    T = k.shape[0]
+    ldv = _tokens("v", v, ck.H, ck.dh, T, k.dtype)
+    _index("pos", pos, (T,))
+    _index("seq", seq, (T,), optional=True)
+    n_heads = 0
+    if heads is not None:
+        _index("heads", heads, (T, None) if not isinstance(heads, torch.Tensor) or heads.dim() != 2 else (T, heads.shape[1]))
+        n_heads = heads.shape[1]
+    ldq = ldqo = Hq = 0
+    mine = q is not None and q_out is None
+    if q is not None:
+        ldq = _tokens("q", q, None, ck.dh, T, k.dtype)
+        Hq = q.shape[1]
+        if mine:
+            # (rows of idle tokens are not written)
+            q_out = torch.zeros((T, Hq, ck.dh), dtype=q.dtype, device=q.device)
+        ldqo = ldq if q_out is q else _tokens("q_out", q_out, Hq, ck.dh, T, k.dtype)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _here(k, v, pos, seq, heads, q, q_out, kv.K, kv.V, kv.table, rotary.freq if rotary is not None else None)
+    _check("dv_paged_append", lib.dv_paged_append(
+        ctypes.byref(ck), ctypes.byref(cr) if cr is not None else None, _ptr(k), ldk, _ptr(v), ldv, _wtype(k), T, _ptr(seq),
+        _ptr(pos), _ptr(heads), n_heads, _ptr(q), ldq, Hq, _ptr(q_out), ldqo, _stream(stream)))
+    if mine:
+        _used_on(stream, q_out)
+    return q_out
+
+
+def paged_attn_workspace_bytes(kv: PagedKV, T, q_heads, max_len, n_heads=0, shared_pages=0) -> int:
+    """Workspace of dv_paged_attn for T tokens; n_heads: heads of a token's set (0: all q_heads)."""
+    ck = kv.c()
+    return load().dv_paged_attn_workspace_bytes(ctypes.byref(ck), T, q_heads, n_heads, max_len, shared_pages)
+
+
+def dv_paged_attn(kv: PagedKV, q, pos, max_len, scale, seq=None, heads=None, q_heads=None, shared_pages=0, out=None,
+                  lse=None, ws=None, flags=0, stream=None):
+    """Decode attention of tokens q [T][n][dh] fp32 over rows 0..pos[t] (< max_len) of their sequences' pages: all
+    q_heads (= n unless given) query heads, or each token's set heads [T][n] of them. shared_pages: leading pages that
+    all sequences share, attended once for the batch. Returns out [T][n][dh], or (out, lse) if lse [T][n]
+    (the log-sum-exp of the logits) is given."""
+    lib = load()
+    ck = kv.c()
+    dh = ck.dh
+    if not (type(q) is torch.Tensor and q.dim() == 3 and _fits(q, torch.float32, (q.shape[0], q.shape[1], dh))):
+        _tensor("q", q, _F32, 3, (None, None, dh))
+    T, n = q.shape[0], q.shape[1]
+    _index("pos", pos, (T,))
+    _index("seq", seq, (T,), optional=True)
+    _index("heads", heads, (T, n), optional=True)
+    if q_heads is None:
+        q_heads = n if heads is None else ck.H
+    if heads is None and q_heads != n:
+        raise ValueError(f"q holds {n} heads of {q_heads}, without a head set")
+    mine = []
+    if out is None:
+        out = torch.empty_like(q)
+        mine.append(out)
+    elif not _fits(out, torch.float32, q.shape):
+        _tensor("out", out, _F32, 3, tuple(q.shape))
+    if lse is not None and not _fits(lse, torch.float32, (T, n)):
+        _tensor("lse", lse, _F32, 2, (T, n))
+    if ws is None:
+        ws = _workspace(lib.dv_paged_attn_workspace_bytes(ctypes.byref(ck), T, q_heads, 0 if heads is None else n,
+                                                          max_len, shared_pages), q.device)
+        mine.append(ws)
+    _here(q, pos, seq, heads, out, lse, ws, kv.K, kv.V, kv.table)
+    _check("dv_paged_attn", lib.dv_paged_attn(
+        ctypes.byref(ck), _ptr(q), T, q_heads, _ptr(heads), 0 if heads is None else n, _ptr(seq), _ptr(pos), max_len,
+        shared_pages, scale, _ptr(out), _ptr(lse), *_wsarg(ws), flags, _stream(stream)))
+    _used_on(stream, *mine)
+    return out if lse is None else (out, lse)
+
+
+def sparse_attn_paged_workspace_bytes(attn: Attn, kv: PagedKV, B, n_heads, max_len, shared_pages=0) -> int:
+    ca, ck = attn.c(), kv.c()
+    return load().dv_sparse_attn_paged_workspace_bytes(ctypes.byref(ca), ctypes.byref(ck), B, n_heads, max_len,
+                                                       shared_pages)
+
+
+def dv_sparse_attn_paged(attn: Attn, x, kv: PagedKV, pos, max_len, heads, scale, rotary: Optional[Rotary] = None,
+                         seq=None, shared_pages=0, out=None, ws=None, flags=0, stream=None):
+    """dv_sparse_attn on a cache in pages: x [B][d] projected for each token's heads [B][n_heads], keys (rotated if
+    `rotary` is given) and values written to row pos[b] of sequence seq[b], rows 0..pos[b] attended, projected out.
+    pos and seq are int32 GPU tensors; a slot with pos < 0 is idle (out = bo)."""
+    lib = load()
+    ca, ck = attn.c(), kv.c()
+    cr = rotary.c() if rotary is not None else None
+    if not _fits_rows(x, ca.d):
+        _tensor("x", x, _F32, 2, (None, ca.d))
+    B = x.shape[0]
+    _tensor("heads", heads, _I32, 2, (B, None))
+    n_heads = heads.shape[1]
+    _index("pos", pos, (B,))
+    _index("seq", seq, (B,), optional=True)
+    mine = []
+    if out is None:
+        out = torch.empty((B, ca.d), dtype=torch.float32, device=x.device)
+        mine.append(out)
+    elif not _fits(out, torch.float32, (B, ca.d)):
+        _tensor("out", out, _F32, 2, (B, ca.d))
+    if ws is None:
+        ws = _workspace(lib.dv_sparse_attn_paged_workspace_bytes(ctypes.byref(ca), ctypes.byref(ck), B, n_heads, max_len,
+                                                                 shared_pages), x.device)
+        mine.append(ws)
+    _here(x, pos, seq, heads, out, ws, attn.Wq, kv.K, kv.V, kv.table, rotary.freq if rotary is not None else None)
+    _check("dv_sparse_attn_paged", lib.dv_sparse_attn_paged(
+        ctypes.byref(ca), _ptr(x), B, ctypes.byref(ck), ctypes.byref(cr) if cr is not None else None, _ptr(seq), _ptr(pos),
+        max_len, shared_pages, _ptr(heads), n_heads, scale, _ptr(out), *_wsarg(ws), flags, _stream(stream)))
+    _used_on(stream, *mine)
+    return out
 
 
 STATIC_SCRATCH_BYTES = 16 << 20   # DV_STATIC_SCRATCH_BYTES

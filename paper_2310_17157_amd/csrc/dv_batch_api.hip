@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "dv_internal.hpp"
+#include "dv_paged.hpp"
 
 namespace dv {
 
@@ -131,6 +132,19 @@ size_t batch_attn_ws(const dv_attn* a, int B, int n_heads) {
   return battn_layout(a, B, n_heads, w, &o);
 }
 
+// The out-projection of the coefficients o.C and its sums: out = resid + bo + sum_{h in S_A^b} H_h W^O_h.
+static dv_status battn_project(const dv_attn* a, const BAttn& o, int B, const float* resid, float* out, hipStream_t hs) {
+  McolsArgs c{};
+  c.d = a->d; c.M = a->WoT; c.list = o.Uh; c.list_count = o.hcnt; c.list_max = a->H; c.dh = a->dh;
+  c.list_range = a->H;
+  c.C = o.C; c.ldc = o.ldc; c.S = o.S2; c.B = B; c.P = o.P2;
+  DV_LAUNCH("oproj", hs, launch_mcols(batch_nb(B), c, hs));
+  ColsFinishArgs e{};
+  e.P = o.P2; e.S = o.S2; e.B = B; e.d = a->d; e.bias = a->bo; e.resid = resid; e.out = out;
+  DV_LAUNCH("oproj_finish", hs, launch_cols_finish(e, hs));
+  return DV_OK;
+}
+
 // Attention of every sequence on x16 (normalised fp16 [NB][Kpad]) for head sets
 // heads[B][n_heads]; out = resid + bo + sum_{h in S_A^b} H_h W^O_h.
 // union_done: the head union (and the heads' places) were built by an earlier launch.
@@ -198,15 +212,7 @@ static dv_status battn_run(const dv_attn* a, const dv_kv* kv, const BAttn& o, in
     af.list = o.Uh; af.hcount = o.hcnt; af.C = o.C; af.ldc = o.ldc;
     DV_LAUNCH("attn_finish", hs, launch_attn_finish(NB, af, hs));
   }
-  McolsArgs c{};
-  c.d = a->d; c.M = a->WoT; c.list = o.Uh; c.list_count = o.hcnt; c.list_max = a->H; c.dh = a->dh;
-  c.list_range = a->H;
-  c.C = o.C; c.ldc = o.ldc; c.S = o.S2; c.B = B; c.P = o.P2;
-  DV_LAUNCH("oproj", hs, launch_mcols(NB, c, hs));
-  ColsFinishArgs e{};
-  e.P = o.P2; e.S = o.S2; e.B = B; e.d = a->d; e.bias = a->bo; e.resid = resid; e.out = out;
-  DV_LAUNCH("oproj_finish", hs, launch_cols_finish(e, hs));
-  return DV_OK;
+  return battn_project(a, o, B, resid, out, hs);
 }
 
 dv_status batch_attn(const dv_attn* a, const float* x, int B, const dv_kv* kv, const int32_t* heads, int n_heads,
@@ -222,6 +228,58 @@ dv_status batch_attn(const dv_attn* a, const float* x, int B, const dv_kv* kv, c
     DV_LAUNCH("xcast_union_heads", hs, launch_cast_union(x, B, batch_nb(B), a->d, o.Kpad, nullptr, nullptr, 0.f, o.X16,
                                                          heads, n_heads, a->H, o.Uh, o.hcnt, nullptr, o.slot, hs));
   return battn_run(a, kv, o, B, heads, n_heads, scale, nullptr, out, hs, true);
+}
+
+// The same on a cache in pages: the fresh keys and values go to a buffer [B][H][dh] (one row a head), from which
+// the append takes them into the pages, and the attention gives one part a head.
+static size_t battn_paged_layout(const dv_attn* a, const dv_paged_kv* kv, int B, int n_heads, int max_len, int shared_pages,
+                                 Workspace& w, BAttn* o, float** k, float** v, char** step) {
+  battn_layout(a, B, n_heads, w, o);
+  *k = w.take<float>((size_t)B * a->H * a->dh * 4);
+  *v = w.take<float>((size_t)B * a->H * a->dh * 4);
+  *step = w.take<char>(paged_step_ws(kv, B, n_heads, max_len, shared_pages));
+  return w.off;
+}
+
+size_t batch_attn_paged_ws(const dv_attn* a, const dv_paged_kv* kv, int B, int n_heads, int max_len, int shared_pages) {
+  Workspace w(nullptr);
+  BAttn o;
+  float *k, *v;
+  char* step;
+  return battn_paged_layout(a, kv, B, n_heads, max_len, shared_pages, w, &o, &k, &v, &step);
+}
+
+dv_status batch_attn_paged(const dv_attn* a, const float* x, int B, const PagedStep& p, const int32_t* heads, int n_heads,
+                           float* out, void* ws, size_t ws_bytes, hipStream_t hs) {
+  Workspace w(ws);
+  BAttn o;
+  float *k, *v;
+  char* step;
+  if (battn_paged_layout(a, p.kv, B, n_heads, p.max_len, p.shared_pages, w, &o, &k, &v, &step) > ws_bytes)
+    return DV_ERR_WORKSPACE;
+  if (n_heads == 0) {
+    ColsFinishArgs e{};
+    e.P = nullptr; e.S = 0; e.B = B; e.d = a->d; e.bias = a->bo; e.out = out;
+    DV_LAUNCH("oproj_finish", hs, launch_cols_finish(e, hs));
+    return DV_OK;
+  }
+  const int NB = batch_nb(B);
+  DV_LAUNCH("xcast_union_heads", hs, launch_cast_union(x, B, NB, a->d, o.Kpad, nullptr, nullptr, 0.f, o.X16, heads,
+                                                       n_heads, a->H, o.Uh, o.hcnt, nullptr, o.slot, hs));
+  RowsArgs r{};
+  RowsSrc& rs = r.src[0];
+  rs.d = a->d; rs.X = o.X16; rs.W0 = a->Wq; rs.W1 = a->Wk; rs.W2 = a->Wv; rs.n0 = a->H * a->dh;
+  rs.list = o.Uh; rs.list_count = o.hcnt; rs.list_max = a->H; rs.list_range = a->H; rs.dh = a->dh;
+  r.B = B; r.slot = o.slot; r.n_heads = n_heads; r.cap = 1;
+  r.bq = a->bq; r.bk = a->bk; r.bv = a->bv; r.q = o.q; r.K = k; r.V = v;
+  DV_LAUNCH("qkv", hs, launch_rows(NB, kEpiQkv, DV_F32, false, r, hs));
+  const dv_status st = paged_step(p, B, heads, n_heads, o.q, k, v, o.part, step, hs);
+  if (st != DV_OK) return st;
+  AttnFinishArgs af{};
+  af.part = o.part; af.n_split = 1; af.n_heads = n_heads; af.dh = a->dh; af.B = B; af.heads = heads;
+  af.list = o.Uh; af.hcount = o.hcnt; af.C = o.C; af.ldc = o.ldc;
+  DV_LAUNCH("attn_finish", hs, launch_attn_finish(NB, af, hs));
+  return battn_project(a, o, B, nullptr, out, hs);
 }
 
 // ---------------------------------------------------------------- layer

@@ -1,0 +1,535 @@
+"""The paged cache on the GPU against the fp64 oracle (oracle.paged), element by element.
+
+Bounds, before any run (u = 2^-24, half a step of fp32):
+  rotation  the angle reaches the sine as an fp32 number of half turns below 1 (off by pi u), sine and cosine by
+            4 ulp (8 u), the factor, two products and a sum by u each: |x0| + |x1| times 16 u mscale, then
+            half a step of the stored type (2^-11 of the value in fp16, 2^-25 at least).
+  logits    queries as two fp16 halves are within 2^-22 of each element, products are exact, and sums of dh terms are
+            within dh u of the sum of magnitudes; the scale's exponent, its product, log2(e) and the argument of
+            the exponential add 4 u of the logit: d = mag (2^-22 + (dh + 5) u), mag the largest sum of
+            |products| of a row's logits.
+  output    weights are off by e^(2 d) - 1 from the logits, 2^-21 from two exponentials (one of a running maximum
+            each) and 2^-22 from two halves; sums over n rows are taken in steps of 32 products by one
+            accumulator, its rescalings and the join: at most n / 32 + 64 roundings: |err| <= sum p |V| (2.1 d +
+            (n / 32 + 80) u) with the halves inside; lse: d + (n / 32 + 80) u + 2^-22 |lse|.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as P
+from paper_2310_17157_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f16": torch.float16, "f32": torch.float32}
+LAYOUT = {"half": B.DV_ROPE_HALF, "interleaved": B.DV_ROPE_INTERLEAVED}
+
+
+def dev(a, dtype=None):
+    t = torch.as_tensor(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def h64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def rounding(y, dtype):
+    return np.maximum(np.abs(y) * 2.0 ** -11, 2.0 ** -25) if dtype == "f16" else np.abs(y) * U
+
+
+def rope_bound(x, freq, layout, mscale, y, dtype):
+    n = len(freq)
+    pair = np.zeros_like(x)
+    if layout == "half":
+        s = np.abs(x[..., :n]) + np.abs(x[..., n:2 * n])
+        pair[..., :n] = pair[..., n:2 * n] = s
+    else:
+        s = np.abs(x[..., 0:2 * n:2]) + np.abs(x[..., 1:2 * n:2])
+        pair[..., 0:2 * n:2] = pair[..., 1:2 * n:2] = s
+    return 16 * U * mscale * pair * (1 + 2.0 ** -10) + rounding(y, dtype)
+
+
+# ------------------------------------------------------------------ rope
+@pytest.mark.parametrize("T,H,dh,rot,layout,dtype,inverse", [
+    (1, 1, 2, 2, "half", "f32", False), (1, 12, 64, 64, "half", "f32", False), (33, 96, 128, 128, "half", "f32", False),
+    (7, 5, 80, 32, "half", "f16", True), (7, 5, 80, 32, "interleaved", "f32", True),
+    (300, 3, 128, 64, "interleaved", "f16", False), (65, 2, 256, 256, "half", "f16", False),
+    (19, 4, 40, 20, "half", "f16", False), (19, 4, 40, 20, "interleaved", "f16", True), (5, 3, 7, 6, "half", "f32", False),
+    (5, 3, 7, 6, "interleaved", "f16", False), (2000, 1, 64, 64, "interleaved", "f32", False),
+    (1, 700, 128, 128, "half", "f16", False)])
+def test_rope(T, H, dh, rot, layout, dtype, inverse):
+    rng = np.random.default_rng(T + dh)
+    freq = P.freqs(rot, rule="parts", factor=8.0, orig_len=4096.0)
+    x = dev(rng.normal(size=(T, H, dh)), DT[dtype])
+    pos = rng.integers(-5, 1 << 20, T).astype(np.int32)
+    pos[0] = 2 ** 31 - 1 if T > 1 else 0
+    rot_ = B.Rotary(dev(freq), LAYOUT[layout], 1.25)
+    out = B.dv_rope(rot_, x, dev(pos), inverse=inverse)
+    want = P.rope(h64(x), pos, freq, layout, 1.25, inverse)
+    err = np.abs(h64(out) - want)
+    # the angle itself: position times frequency is exact to 2^-53 of up to 2^31 radians, 2.4e-7
+    slack = np.abs(pos[:, None, None].astype(float)) * 2.0 ** -52 * (np.abs(h64(x)).max() * 2.5)
+    assert (err <= rope_bound(h64(x), freq, layout, 1.25, want, dtype) + slack).all(), err.max()
+    again = B.dv_rope(rot_, x, dev(pos), inverse=inverse)
+    assert torch.equal(out, again)
+    B.dv_rope(rot_, x, dev(pos), inverse=inverse, out=x)          # in place
+    assert torch.equal(out, x)
+
+
+def test_rope_strided_unaligned_and_empty():
+    """A slice of a fused projection, an odd element offset (the narrow path), no tokens; what lies between tokens
+    is left as it was."""
+    freq = P.freqs(16)
+    r = B.Rotary(dev(freq))
+    pos = dev(np.array([3, 900000, 0, 17], dtype=np.int32))
+    for off, width in ((0, 5 * 16), (16, 7 * 16), (3, 101)):
+        base = torch.randn(4, width + 16, dtype=torch.float16, device="cuda")
+        x = base[:, off:off + 48].view(4, 3, 16) if width != 101 else base.as_strided((4, 3, 16), (width + 16, 16, 1), 3)
+        out = torch.full((4, 200), 7.0, dtype=torch.float16, device="cuda")
+        o = out.as_strided((4, 3, 16), (200, 16, 1), off)
+        B.dv_rope(r, x, pos, out=o)
+        want = P.rope(h64(x), pos.cpu().numpy(), freq)
+        slack = 9e5 * 2.0 ** -52 * 10
+        assert (np.abs(h64(o) - want) <= rope_bound(h64(x), freq, "half", 1.0, want, "f16") + slack).all()
+        o.fill_(7.0)
+        assert (out == 7.0).all()
+    assert B.dv_rope(r, torch.zeros(0, 3, 16, device="cuda"), pos[:0]).shape == (0, 3, 16)
+
+
+def test_rope_inverse_is_the_gradient():
+    """<w, rope(x)> rises along the inverse rotation of w (fp32 differences of a linear map: exact up to
+    roundings), and the inverse undoes the rotation."""
+    r = B.Rotary(dev(P.freqs(32)), B.DV_ROPE_INTERLEAVED, 1.5)
+    x, w = torch.randn(9, 4, 48, device="cuda"), torch.randn(9, 4, 48, device="cuda")
+    e = torch.randn(9, 4, 48, device="cuda")
+    pos = torch.arange(9, dtype=torch.int32, device="cuda") * 1000
+    f = lambda v: (B.dv_rope(r, v, pos).double() * w.double()).sum()
+    g = B.dv_rope(r, w, pos, inverse=True)
+    d = (f(x + e) - f(x - e)) / 2
+    assert abs(d - (g.double() * e.double()).sum()) <= 64 * U * 2.25 * (w.double().abs().sum() * 6)
+    y = B.dv_rope(B.Rotary(dev(P.freqs(32))), x, pos)
+    back = B.dv_rope(B.Rotary(dev(P.freqs(32))), y, pos, inverse=True)
+    assert (back - x).abs().max() <= 64 * U * x.abs().max()
+
+
+# ------------------------------------------------------------------ cache
+def pool(rng, n_pages, H, page, dh, dtype, order="head"):
+    """K, V as views of one allocation, in head-major or row-major pages."""
+    if order == "head":
+        t = dev(rng.normal(size=(n_pages, 2, H, page, dh)), DT[dtype])
+        return t, t[:, 0], t[:, 1]
+    t = dev(rng.normal(size=(n_pages, page, 2, H, dh)), DT[dtype])
+    return t, t[:, :, 0].transpose(1, 2), t[:, :, 1].transpose(1, 2)
+
+
+def block_table(rng, n_pages, counts, shared=0):
+    perm = rng.permutation(n_pages)
+    width = shared + max(list(counts) + [1])
+    table = np.full((len(counts), width), 10 ** 9, dtype=np.int32)      # (never read beyond a sequence's pages)
+    table[:, :shared] = perm[:shared]
+    at = shared
+    for s, c in enumerate(counts):
+        table[s, shared:shared + c] = perm[at:at + c]
+        at += c
+    assert at <= n_pages
+    return table
+
+
+@pytest.mark.parametrize("H,Hq,dh,page,ktype,xtype,layout,rot,order,sets", [
+    (1, 1, 8, 1, "f16", "f32", "half", 8, "head", 0), (12, 12, 64, 16, "f32", "f32", "half", 64, "head", 0),
+    (8, 64, 128, 64, "f16", "f16", "interleaved", 128, "row", 0), (7, 0, 56, 10, "f32", "f16", None, 0, "head", 0),
+    (5, 15, 80, 24, "f16", "f16", "half", 20, "row", 0), (96, 32, 128, 16, "f16", "f32", "half", 128, "head", 32),
+    (10, 4, 40, 7, "f16", "f32", "interleaved", 10, "head", 3), (2, 2, 256, 5, "f32", "f32", None, 0, "row", 1)])
+def test_append(H, Hq, dh, page, ktype, xtype, layout, rot, order, sets):
+    rng = np.random.default_rng(H * dh)
+    lens = [3, 0, 21, 1, 6]
+    start = [0, 4, 2 * page - 1 if page > 1 else 2, 5, 11]
+    n_pages = sum((s + n) // page + 1 for s, n in zip(start, lens)) + 2
+    table = block_table(rng, n_pages, [(s + n) // page + 1 for s, n in zip(start, lens)])
+    whole, K, V = pool(rng, n_pages, H, page, dh, ktype, order)
+    pos = np.concatenate([s + np.arange(n) for s, n in zip(start, lens)] + [[-1, -7]]).astype(np.int32)
+    seq = np.concatenate([np.full(n, i) for i, n in enumerate(lens)] + [[1, 10 ** 6]]).astype(np.int32)
+    mix = rng.permutation(len(pos))
+    pos, seq = pos[mix], seq[mix]
+    T = len(pos)
+    fused = dev(rng.normal(size=(T, (Hq + 2 * H) * dh + 8)), DT[xtype])
+    q, k, v = (fused[:, a * dh:(a + n) * dh].view(T, n, dh) for a, n in ((0, Hq), (Hq, H), (Hq + H, H)))
+    heads = np.stack([np.sort(rng.permutation(H)[:sets]) for _ in range(T)]).astype(np.int32) if sets else None
+    K0, V0, W0 = h64(K), h64(V), whole.clone()
+    freq = P.freqs(rot) if rot else None
+    r = B.Rotary(dev(freq), LAYOUT[layout]) if rot else None
+    qo = torch.full((T, Hq, dh), 9.0, dtype=DT[xtype], device="cuda") if Hq else None
+    got = B.dv_paged_append(B.PagedKV(K, V, dev(table)), k, v, dev(pos), seq=dev(seq), rotary=r,
+                            heads=None if heads is None else dev(heads), q=q if Hq else None, q_out=qo)
+    turn = lambda x: P.rope(x, np.maximum(pos, 0), freq, layout) if rot else x
+    kr, live = turn(h64(k)), pos >= 0
+    bound_k = rope_bound(h64(k), freq, layout, 1.0, kr, ktype) if rot else rounding(kr, ktype)
+    wantK, wantV = (P.append(x0, x, table, seq, pos, heads) for x0, x in ((K0, kr), (V0, h64(v))))
+    tolK = P.append(np.zeros_like(K0), bound_k, table, seq, pos, heads)
+    assert (np.abs(h64(K) - wantK) <= tolK).all()                    # 0 where nothing was appended
+    assert (np.abs(h64(V) - wantV) <= np.where(wantV == V0, 0, rounding(wantV, ktype))).all()
+    touched = (whole != W0).sum().item()
+    assert touched <= 2 * live.sum() * (sets or H) * dh
+    if Hq:
+        assert got is qo
+        want = turn(h64(q))
+        tol = rope_bound(h64(q), freq, layout, 1.0, want, xtype) if rot else 0 * want
+        assert (np.abs(h64(qo) - want) <= tol)[live].all()
+        assert (qo[torch.from_numpy(~live).cuda()] == 9.0).all()      # idle tokens' queries are left out
+        if T > 2:
+            B.dv_paged_append(B.PagedKV(K, V, dev(table)), k.clone(), v, dev(pos), seq=dev(seq), rotary=r, q=q, q_out=q,
+                              heads=None if heads is None else dev(heads))
+            assert torch.equal(q[torch.from_numpy(live).cuda()], qo[torch.from_numpy(live).cuda()])
+
+
+def test_append_writes_nothing_out_of_range():
+    """A bad sequence, row, page or head writes nothing anywhere (checked by the kernel before it forms an
+    address); the other tokens are appended."""
+    rng = np.random.default_rng(4)
+    _, K, V = pool(rng, 4, 2, 8, 16, "f16")
+    K0 = K.clone()
+    table = dev(np.array([[0, 99], [-1, 1]], dtype=np.int32))
+    k = torch.ones(7, 2, 16, device="cuda")
+    pos = dev(np.array([1, 9, 2, 9, 16, 3, 2 ** 31 - 1], dtype=np.int32))
+    seq = dev(np.array([0, 0, 1, 1, 0, 2, 0], dtype=np.int32))
+    B.dv_paged_append(B.PagedKV(K, V, table), k, k, pos, seq=seq)
+    want = K0.clone()
+    want[0, :, 1] = 1.0
+    want[1, :, 1] = 1.0
+    assert torch.equal(K, want)
+    heads = dev(np.array([[-1], [2], [0], [1], [0], [0], [0]], dtype=np.int32))
+    K.copy_(K0)
+    B.dv_paged_append(B.PagedKV(K, V, table), k, k, pos, seq=seq, heads=heads)
+    want = K0.clone()
+    want[1, 1, 1] = 1.0
+    assert torch.equal(K, want)
+
+
+# ------------------------------------------------------------------ attention
+def make(rng, lens, H, G, dh, page, ktype, tokens=1, shared=0, order="head", sets=0, junk=math.nan, qmag=1.5):
+    """Sequences of shared * page + lens[s] rows, `tokens` query tokens each; rows behind a sequence's last token and
+    unused pages hold `junk`."""
+    counts = [-(-n // page) for n in lens]
+    n_pages = shared + sum(counts) + 2
+    table = block_table(rng, n_pages, counts, shared)
+    P0 = shared * page
+    _, K, V = pool(rng, n_pages, H, page, dh, ktype, order)
+    used = np.zeros((n_pages, page), dtype=bool)
+    if P0 and any(n > 0 for n in lens):
+        used[table[0, :shared]] = True
+    for s, n in enumerate(lens):
+        for p in range(n):
+            used[table[s, shared + p // page], p % page] = True
+    hide = torch.from_numpy(~used).cuda()[:, None, :, None]
+    K.masked_fill_(hide, junk)
+    V.masked_fill_(hide, junk)
+    pos = np.concatenate([P0 + n - tokens + np.arange(tokens) for n in lens]).astype(np.int32)
+    pos = np.maximum(pos, -1)
+    seq = np.repeat(np.arange(len(lens)), tokens).astype(np.int32)
+    n = sets or H * G
+    heads = np.stack([np.sort(rng.permutation(H * G)[:n]) for _ in pos]).astype(np.int32) if sets else None
+    q = (rng.normal(size=(len(pos), n, dh)) * qmag).astype(np.float32)
+    return dict(K=K, V=V, table=table, pos=pos, seq=seq, heads=heads, q=q, G=G, dh=dh, H=H, shared=shared, page=page)
+
+
+def attend(c, scale=None, max_len=None, shared=None, lse=True, **kw):
+    kv = B.PagedKV(c["K"], c["V"], dev(np.minimum(c["table"], 2 ** 31 - 1)))
+    scale = 1 / math.sqrt(c["dh"]) if scale is None else scale
+    width = c["table"].shape[1] * c["page"]
+    l = torch.full(c["q"].shape[:2], 5.0, device="cuda") if lse else None
+    return B.dv_paged_attn(kv, dev(c["q"]), dev(c["pos"]), max_len or min(width, max(1, int(c["pos"].max()) + 1)), scale,
+                           seq=dev(c["seq"]), heads=None if c["heads"] is None else dev(c["heads"]), q_heads=c["H"] * c["G"],
+                           shared_pages=c["shared"] if shared is None else shared, lse=l, **kw)
+
+
+def check(c, out, lse, scale=None):
+    scale = 1 / math.sqrt(c["dh"]) if scale is None else scale
+    o, l, mag, absv = P.attn(c["q"], h64(c["K"]), h64(c["V"]), c["table"], c["seq"], c["pos"], scale, c["G"], c["heads"])
+    n = np.maximum(c["pos"] + 1, 0)[:, None]
+    d = mag * (2.0 ** -22 + (c["dh"] + 5) * U)
+    steps = (n / 32 + 80) * U
+    err = np.abs(h64(out) - o)
+    assert (err <= absv * (2.1 * d + steps)[..., None]).all(), (err / np.maximum(absv, 1e-30)).max()
+    live = c["pos"] >= 0
+    got = h64(lse)
+    assert np.isneginf(got[~live]).all()
+    l = np.where(live[:, None], l, 0.0)
+    got = np.where(live[:, None], got, 0.0)
+    assert (np.abs(got - l)[live] <= (d + steps + 2.0 ** -22 * np.abs(l))[live]).all()
+
+
+CASES = [
+    # lens, H, G, dh, page, ktype, tokens, shared, order, sets
+    ([1], 1, 1, 8, 1, "f16", 1, 0, "head", 0),
+    ([1, 2, 31, 32, 33, 127, 128, 129], 3, 1, 64, 16, "f16", 1, 0, "head", 0),
+    ([128], 12, 1, 64, 16, "f32", 1, 0, "head", 0),
+    ([0, 5, 300, 0, 1025], 2, 4, 128, 24, "f16", 2, 0, "row", 0),
+    ([700, 3], 2, 8, 128, 64, "f16", 1, 0, "head", 0),
+    ([77, 200], 1, 15, 80, 7, "f16", 1, 0, "head", 0),
+    ([90, 150], 1, 71, 40, 10, "f16", 1, 0, "row", 0),
+    ([130, 513], 2, 3, 56, 10, "f32", 3, 0, "row", 0),
+    ([40, 260], 1, 20, 96, 16, "f32", 1, 0, "head", 0),
+    ([64, 300], 2, 1, 256, 16, "f16", 1, 0, "head", 0),
+    ([64, 300], 1, 12, 192, 16, "f16", 1, 0, "row", 0),
+    ([50, 300], 2, 2, 256, 5, "f32", 1, 0, "head", 0),
+    ([50, 70], 1, 40, 200, 5, "f32", 1, 0, "head", 0),
+    ([600, 20, 333], 10, 1, 128, 16, "f16", 1, 0, "head", 4),
+    ([200, 20, 333], 3, 4, 128, 16, "f16", 1, 0, "head", 5),
+    ([200, 20], 2, 24, 64, 16, "f16", 1, 0, "row", 40),
+    ([90, 20, 33], 6, 1, 64, 8, "f32", 2, 0, "head", 2),
+    ([9000], 1, 2, 64, 128, "f16", 1, 0, "head", 0),
+    # a prefix that all share
+    ([1, 40, 200], 2, 1, 128, 16, "f16", 1, 8, "head", 0),
+    ([0, 3, 200, 17, 1, 60, 5, 8, 9, 10, 11, 12], 3, 1, 64, 16, "f16", 1, 20, "row", 0),
+    ([5, 40] * 8, 2, 4, 128, 16, "f16", 1, 9, "head", 0),
+    ([5, 40] * 4, 1, 4, 128, 7, "f16", 3, 50, "head", 0),
+    ([2, 40, 0, 8, 100, 33, 3, 1], 1, 3, 64, 10, "f16", 4, 30, "head", 0),
+    ([30, 4, 200], 10, 1, 80, 16, "f16", 1, 12, "head", 4),
+    ([30, 4] * 15, 6, 2, 64, 16, "f16", 1, 12, "head", 5),
+    ([30, 4, 99], 2, 3, 56, 10, "f32", 2, 13, "row", 0),
+    ([30, 4] * 10, 1, 3, 128, 10, "f32", 1, 13, "head", 0),
+    ([30, 4] * 3, 1, 8, 256, 16, "f16", 1, 20, "head", 0),
+    ([30, 4] * 3, 1, 8, 256, 16, "f32", 1, 20, "head", 0),
+    ([3, 1], 2, 1, 64, 16, "f16", 1, 300, "head", 0),
+]
+
+
+@pytest.mark.parametrize("lens,H,G,dh,page,ktype,tokens,shared,order,sets", CASES)
+def test_attention(lens, H, G, dh, page, ktype, tokens, shared, order, sets):
+    """Everything behind a token's last row is NaN, table entries behind its pages are out of range."""
+    rng = np.random.default_rng(len(lens) * dh + H)
+    c = make(rng, lens, H, G, dh, page, ktype, tokens, shared, order, sets)
+    out, lse = attend(c)
+    check(c, out, lse)
+    again, _ = attend(c)
+    assert torch.equal(out, again)
+    assert torch.equal(attend(c, lse=False), out)
+    # a larger bound of the rows cuts the work otherwise, with the same result up to roundings
+    width = c["table"].shape[1] * page
+    if width > int(c["pos"].max()) + 1:
+        out, lse = attend(c, max_len=width)
+        check(c, out, lse)
+    if shared:                                          # the shared rows are a hint: without it, the same
+        out, lse = attend(c, shared=0)
+        check(c, out, lse)
+
+
+@pytest.mark.parametrize("ktype", ["f16", "f32"])
+@pytest.mark.parametrize("junk", [math.inf, -65504.0, 65504.0])
+def test_attention_last_row_counts_and_the_next_does_not(ktype, junk):
+    """The last row holds most of the weight (its key is the query), the row behind it an infinity or the largest
+    value: an end off by one shows at once."""
+    rng = np.random.default_rng(8)
+    lens = [1, 16, 17, 32, 33, 64, 100, 128, 129, 160, 161]
+    c = make(rng, lens, 2, 1, 64, 16, ktype, junk=junk)
+    for t, n in enumerate(lens):
+        g, r = c["table"][t, (n - 1) // 16], (n - 1) % 16
+        c["K"][int(g), :, r] = dev(c["q"][t]).to(c["K"].dtype) * 1.5
+    out, lse = attend(c)
+    check(c, out, lse)
+
+
+def test_attention_values_of_all_sizes():
+    """Queries from 1e-30 to 1e30 with keys that cancel their size, one large element beside small ones, zero and
+    subnormal values, a negative and a zero scale."""
+    rng = np.random.default_rng(9)
+    c = make(rng, [200] * 6, 1, 1, 64, 16, "f16")
+    for t, m in enumerate([1e-30, 1e30, 1.0, 1.0, 0.0, 1e-42]):
+        c["q"][t] *= np.float32(m)
+    c["q"][2, 0, 5] = 3000.0
+    c["K"][..., 5] *= 2.0 ** -12
+    c["V"].mul_(2.0 ** -14)
+    for scale in (0.125, -0.125, 0.0):
+        keep = c["q"][1].copy()
+        if scale:
+            c["q"][1] = np.float32(0)
+        out, lse = attend(c, scale=scale)
+        c2 = dict(c)
+        # stored fp16 values near their smallest: the output's own bound holds with them as they are
+        check(c2, out, lse, scale=scale)
+        c["q"][1] = keep
+    c["q"][:] = 1e30 * np.sign(c["q"])
+    out, lse = attend(c, scale=1e-31)
+    check(c, out, lse, scale=1e-31)
+
+
+def test_attention_non_finite_stays_with_its_head():
+    """An infinite key or NaN value in an attended row reaches the outputs of that head and sequence alone."""
+    rng = np.random.default_rng(10)
+    for shared in (0, 6):
+        c = make(rng, [40, 90, 33], 2, 2, 64, 16, "f16", shared=shared)
+        g = int(c["table"][1, shared + 2])
+        c["V"][g, 1, 3, 7] = math.nan
+        c["K"][g, 1, 4, 0] = math.inf
+        out, lse = attend(c)
+        bad = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+        bad[1, 2:] = True
+        assert torch.equal(out.isfinite().all(dim=-1), ~bad)
+        good = ~bad.cpu().numpy()
+        c["V"][g, 1, 3, 7] = 0.0
+        c["K"][g, 1, 4, 0] = 0.0
+        o, _, _, absv = P.attn(c["q"], h64(c["K"]), h64(c["V"]), c["table"], c["seq"], c["pos"], 0.125, 2)
+        assert (np.abs(h64(out) - o)[good] <= 1e-4 * absv[good]).all()
+
+
+def test_attention_same_pages_and_tokens_twice():
+    """Two slots of one sequence, a page twice in one row, the same head twice in a set: each is computed."""
+    rng = np.random.default_rng(11)
+    c = make(rng, [100, 64], 4, 1, 64, 16, "f16", sets=3)
+    c["table"][1, 1] = c["table"][1, 0]
+    c["seq"][:] = 1
+    c["pos"][:] = [63, 40]
+    c["heads"][0] = [2, 2, 3]
+    c["heads"][1] = [3, 0, 0]
+    out, lse = attend(c, shared=0)
+    check(c, out, lse)
+    c["pos"][:] = [63, 47]
+    out, lse = attend(c, shared=2)                     # (one sequence: its pages are the shared ones)
+    check(c, out, lse)
+
+
+def test_attention_validate():
+    rng = np.random.default_rng(12)
+    c = make(rng, [30, 70, 0], 2, 1, 64, 16, "f16", shared=3)
+    out, lse = attend(c, flags=B.DV_VALIDATE)
+    check(c, out, lse)
+
+    def refused(**kw):
+        d = {k: (v.copy() if isinstance(v, np.ndarray) else v) for k, v in c.items()}
+        max_len = None
+        for k, f in kw.items():
+            if k == "max_len":
+                max_len = f
+            else:
+                f(d)
+        with pytest.raises(B.DvError) as e:
+            attend(d, flags=B.DV_VALIDATE, max_len=max_len)
+        return e.value.status == B.DV_ERR_INDEX
+
+    assert refused(a=lambda d: d["table"].__setitem__((1, 4), -1))
+    assert refused(a=lambda d: d["table"].__setitem__((0, 0), d["K"].shape[0]))
+    assert refused(a=lambda d: d["table"].__setitem__((1, 2), d["table"][1, 1]))       # not the shared page
+    assert refused(a=lambda d: d["seq"].__setitem__(0, 3))
+    assert refused(max_len=100)                                                          # pos >= max_len
+    c["seq"][2] = 99                                                                     # pos: an idle slot, its sequence unused
+    c["pos"][2] = -1
+    attend(c, flags=B.DV_VALIDATE)
+
+
+def test_clamped_pages_and_positions_do_not_fault():
+    """Out-of-range entries without DV_VALIDATE are clamped: some result, tokens that have good ones right."""
+    rng = np.random.default_rng(13)
+    c = make(rng, [30, 70], 2, 1, 64, 16, "f16", junk=0.0)
+    good, _ = attend(c)
+    c["table"][0, 0], c["table"][0, 1] = -5, 10 ** 8
+    c["seq"][0] = 0
+    out, _ = attend(c)
+    assert torch.equal(out[1], good[1])
+    c["pos"][0], c["seq"][0] = 2 ** 31 - 1, -9
+    out, _ = attend(c, max_len=80)
+    check(dict(c, q=c["q"][1:], pos=c["pos"][1:], seq=c["seq"][1:]), out[1:], attend(c, max_len=80)[1][1:])
+
+
+# ------------------------------------------------------------------ offsets past 32 bits
+def test_pages_past_four_gigabytes():
+    """A pool of 9 GB (bytes past 2^33), the used pages at its end."""
+    n_pages, H, page, dh = 1100, 16, 1024, 128
+    pool_ = torch.empty((n_pages, 2, H, page, dh), dtype=torch.float16, device="cuda")
+    K, V = pool_[:, 0], pool_[:, 1]
+    rng = np.random.default_rng(14)
+    table = np.array([[n_pages - 1, 3, n_pages - 2]], dtype=np.int32)
+    for g in table[0]:
+        K[int(g)].normal_()
+        V[int(g)].normal_()
+    kv = B.PagedKV(K, V, dev(table))
+    k = torch.randn(1, H, dh, device="cuda")
+    pos = dev(np.array([2500], dtype=np.int32))
+    B.dv_paged_append(kv, k, k, pos)
+    assert torch.equal(K[n_pages - 2, :, 2500 - 2048], k[0].half())
+    q = torch.randn(1, H, dh, device="cuda")
+    out = B.dv_paged_attn(kv, q, pos, 3072, 0.1)
+    Kd, Vd = (torch.cat([X[int(g)] for g in table[0]], dim=1)[:, :2501].double() for X in (K, V))
+    s = (Kd @ q[0].double()[:, :, None]).squeeze(-1) * 0.1
+    want = (torch.softmax(s, dim=-1)[:, None] @ Vd).squeeze(1)
+    assert (out[0].double() - want).abs().max() <= 1e-5
+
+
+# ------------------------------------------------------------------ streams, graphs
+def test_other_stream_and_captured_steps():
+    """A decode step (append with rotation, attention) captured once and replayed with new tokens as the sequences grow,
+    two graphs over one workspace among eager calls; each replay against the eager calls on another stream."""
+    rng = np.random.default_rng(15)
+    H, G, dh, page, n_seq, steps = 2, 4, 64, 16, 3, 5
+    table = dev(block_table(rng, 24, [6, 6, 6], 2))
+    pools = [pool(np.random.default_rng(16), 24, H, page, dh, "f16")[1:] for _ in range(2)]
+    rot = B.Rotary(dev(P.freqs(dh)))
+    kvs = [B.PagedKV(K, V, table) for K, V in pools]
+    st = dict(qkv=torch.zeros(n_seq, (G * H + 2 * H) * dh, device="cuda"), pos=torch.zeros(n_seq, dtype=torch.int32, device="cuda"))
+    cut = lambda a, n: st["qkv"][:, a * dh:(a + n) * dh].view(n_seq, n, dh)
+    ws = torch.empty(B.paged_attn_workspace_bytes(kvs[0], n_seq, G * H, 8 * page, shared_pages=2), dtype=torch.uint8, device="cuda")
+
+    def step(kv, out, **kw):
+        q = torch.empty(n_seq, G * H, dh, device="cuda") if "qbuf" not in kw else kw.pop("qbuf")
+        B.dv_paged_append(kv, cut(G * H, H), cut(G * H + H, H), st["pos"], rotary=rot, q=cut(0, G * H), q_out=q, **kw)
+        B.dv_paged_attn(kv, q, st["pos"], 8 * page, 0.125, shared_pages=2, out=out, ws=ws if not kw else None, **kw)
+
+    outs = [torch.zeros(n_seq, G * H, dh, device="cuda") for _ in range(3)]
+    qbuf = torch.empty(n_seq, G * H, dh, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for kv in kvs:                                     # (the warm-up appends too: to both)
+        step(kv, outs[0], qbuf=qbuf)
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(kvs[0], outs[i], qbuf=qbuf)
+        graphs.append(g)
+    for i in range(steps):
+        st["qkv"].normal_()
+        st["pos"].copy_(dev(np.array([32 + 7 * i, 31 + i if i != 2 else -1, 90 + i], dtype=np.int32)))
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        side.wait_stream(torch.cuda.current_stream())
+        step(kvs[1], outs[2], stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[2]), i
+        assert torch.equal(pools[0][0], pools[1][0]) and torch.equal(pools[0][1], pools[1][1])
+
+
+def test_decode_run_of_all_operators():
+    """Prompts appended at once, then tokens one by one with the shared prefix, against the oracle on the fp64
+    cache that it keeps itself (its keys and values rounded as stored)."""
+    rng = np.random.default_rng(17)
+    H, G, dh, page, shared = 2, 2, 64, 8, 3
+    freq = P.freqs(32, rule="linear", factor=2.0)
+    rot = B.Rotary(dev(freq), B.DV_ROPE_INTERLEAVED)
+    table = block_table(rng, 30, [8, 8], shared)
+    K, V = (torch.zeros(30, H, page, dh, dtype=torch.float16, device="cuda") for _ in range(2))
+    kv = B.PagedKV(K, V, dev(table))
+    lens = [shared * page + 13, shared * page + 30]
+    # the shared prompt through sequence 0, each sequence's own part through its own
+    pos = np.concatenate([np.arange(shared * page)] + [np.arange(shared * page, n) for n in lens]).astype(np.int32)
+    seq = np.concatenate([np.zeros(shared * page), np.zeros(13), np.ones(30)]).astype(np.int32)
+    k, v = (rng.normal(size=(len(pos), H, dh)).astype(np.float32) for _ in range(2))
+    B.dv_paged_append(kv, dev(k), dev(v), dev(pos), seq=dev(seq), rotary=rot)
+    K64 = P.append(np.zeros(K.shape), P.rope(k, pos, freq, "interleaved"), table, seq, pos)
+    for i in range(6):
+        p = np.array([n + i for n in lens], dtype=np.int32)
+        q, k, v = (rng.normal(size=(2, n, dh)).astype(np.float32) for n in (H * G, H, H))
+        qo = B.dv_paged_append(kv, dev(k), dev(v), dev(p), rotary=rot, q=dev(q))
+        K64 = P.append(K64, P.rope(k, p, freq, "interleaved"), table, [0, 1], p)
+        out = B.dv_paged_attn(kv, qo, dev(p), 80, 0.125, shared_pages=shared)
+        kstep = np.abs(h64(K) - K64)
+        assert (kstep <= np.abs(K64) * 2.0 ** -11 + 2.0 ** -20).all()
+        want, _, mag, absv = P.attn(P.rope(q, p, freq, "interleaved"), K64, h64(V), table, [0, 1], p, 0.125, G)
+        # stored keys are off by 2^-11: logits by mag 2^-11
+        assert (np.abs(h64(out) - want) <= absv * (2.2 * mag * 2.0 ** -11 + 1e-4)[..., None]).all()
