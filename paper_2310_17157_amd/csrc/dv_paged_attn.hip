@@ -20,8 +20,10 @@
 // nothing is left). With up to 8 query rows the second halves are columns 8..15 of the same products, so they
 // cost nothing; with more they are products of their own. fp32 caches use the fp32 matrix instructions.
 //
-// Memory bounds it: at one query row per key head the matrix cores are busy about 4 % of the time. So the next
-// step's keys and values are in registers in flight while one is used, page indices two steps ahead.
+// Memory bounds it: at one query row per key head the matrix cores are busy about 4 % of the time. So a step's keys
+// are loaded into the registers of the last step's as soon as its logits are taken, its values as soon as the last
+// value product is, page indices two steps ahead: every wavefront has one to two steps' worth of loads in flight
+// from one set of registers, and more wavefronts fit than with two sets.
 #include <math.h>
 
 #include <type_traits>
@@ -31,6 +33,7 @@
 namespace dv {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPaNW = 4, kPaNT = 64 * kPaNW;
 constexpr float kPaLn2 = 0.693147180559945309f;
@@ -60,7 +63,7 @@ struct PaShape {
   static constexpr int CH = F16 ? (DH == 64 ? 4 : 8) : 4;   // elements of a lane's chunk of a value
   static constexpr int M = DH / (16 * CH);            // chunks of a lane
   static constexpr int DHP = DH + 4;                  // LDS row of the join
-  static constexpr bool DB = DH < 256 || QT == 0;     // two register sets for keys and values
+  static constexpr int WAVES = DH == 64 ? (QT == 0 ? 4 : QT == 2 ? 3 : 2) : DH == 128 ? (QT == 0 ? 3 : QT == 2 ? 2 : 1) : 1;
   static constexpr size_t lds() { return (size_t)kPaNW * RT * (DHP + 2) * sizeof(float); }
 };
 
@@ -70,6 +73,17 @@ __device__ __forceinline__ void pa_wave_sync() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Lane l and l ^ 8 of a row of 16; the maximum over the lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float pa_xor8(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x128, 0xf, 0xf, false));   // row_ror:8
+}
+__device__ __forceinline__ float pa_max_groups(float v) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // Product of a tile: acc += A B.
@@ -83,7 +97,7 @@ __device__ __forceinline__ f32x4 pa_mfma4(f32x4 a, f32x4 b, f32x4 c) {
 }
 
 template <typename KT, int DH, int QT>
-__global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_attn(PagedAttnArgs a) {
   using Sh = PaShape<KT, DH, QT>;
   constexpr bool F16 = Sh::F16, SPLIT = Sh::SPLIT;
   constexpr int NT = Sh::NT, RT = Sh::RT, SK = Sh::SK, KS = Sh::KS, CH = Sh::CH, M = Sh::M, DHP = Sh::DHP;
@@ -190,12 +204,10 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
     offs[wave][buf][lane & (SK - 1)] = min(max(id, 0), a.g.n_pages - 1) * a.g.ps + row * a.g.rs;
   };
   using VT = typename std::conditional<F16 && CH == 4, u32x2, u32x4>::type;
-  struct Step {
-    u32x4 k[SK / 16][KS];
-    VT v[NK][M];
-  };
+  u32x4 kr[SK / 16][KS];
+  VT vr[NK][M];
   // (pieces past the head width read its last bytes: their queries are zero, their outputs not written)
-  auto load = [&](Step& st, int buf) {
+  auto load_k = [&](int buf) {
     pa_wave_sync();
 #pragma unroll
     for (int u = 0; u < SK / 16; ++u) {
@@ -203,28 +215,32 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         const char* pp = p + min(ks * 64 + grp * 16, rowb - 16);
-        st.k[u][ks] = QT == 0 ? ld_stream(pp) : ld_plain(pp);
+        kr[u][ks] = QT == 0 ? ld_stream(pp) : ld_plain(pp);
       }
     }
+  };
+  auto load_v = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < NK; ++i) {
       const char* p = Vh + offs[wave][buf][(i >> 2) * 16 + grp * 4 + (i & 3)];
 #pragma unroll
       for (int m = 0; m < M; ++m) {
         const VT* pp = reinterpret_cast<const VT*>(p + min((m * 16 + col) * (int)sizeof(VT), rowb - (int)sizeof(VT)));
-        st.v[i][m] = QT == 0 ? __builtin_nontemporal_load(pp) : *pp;
+        vr[i][m] = QT == 0 ? __builtin_nontemporal_load(pp) : *pp;
       }
     }
   };
   int id1 = 0;
-  Step sa, sb;
   if (nsteps > 0) {
     place(0, page_load(0), 0);
     if (nsteps > 1) id1 = page_load(1);
-    if constexpr (Sh::DB) load(sa, 0);
+    load_k(0);
+    load_v(0);
   }
 
-  // ---- queries: scaled halves (fp16) or as they are, and the factor from products to base-2 logits
+  // ---- queries: scaled halves (fp16) or as they are, and the factor >= 0 from products to base-2 logits (a negative
+  // scale's sign goes to the queries)
+  const float sign = a.scale < 0.f ? -1.f : 1.f;
   u32x4 qh[NT][KS], ql[NT][SPLIT || !F16 ? 1 : KS];
   float cf[NT];
 #pragma unroll
@@ -252,13 +268,13 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
       mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
       mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
       const int ex = 14 - ((int)((__float_as_uint(mx) >> 23) & 255u) - 127);   // largest element to [2^14, 2^15)
-      cf[nt] = ldexpf(a.scale, -ex);
+      cf[nt] = ldexpf(fabsf(a.scale), -ex);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         f16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float v = ldexpf(x[ks][e >> 2][e & 3], ex);
+          const float v = ldexpf(sign * x[ks][e >> 2][e & 3], ex);
           hi[e] = (_Float16)v;
           lo[e] = (_Float16)(v - (float)hi[e]);
         }
@@ -270,9 +286,9 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
         }
       }
     } else {
-      cf[nt] = a.scale;
+      cf[nt] = fabsf(a.scale);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qh[nt][ks] = __builtin_bit_cast(u32x4, x[ks][0]);
+      for (int ks = 0; ks < KS; ++ks) qh[nt][ks] = __builtin_bit_cast(u32x4, x[ks][0] * sign);
     }
   }
 
@@ -286,49 +302,50 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < M * CH; ++e) o[nt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  auto use = [&](Step& st, int i) {
+  for (int i = 0; i < nsteps; ++i) {
     const int base = key_of(i);
     const bool tail = base + SK > k1;
-    if (tail) {                                        // values behind the last row may be anything
+    f32x4 s[NT][SK / 16];
 #pragma unroll
-      for (int k = 0; k < NK; ++k)
-        if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= k1)
+    for (int nt = 0; nt < NT; ++nt) {
+      if (nt > 0 && nt * 16 >= nr) break;
 #pragma unroll
-          for (int mm = 0; mm < M; ++mm) st.v[k][mm] = VT{};
+      for (int u = 0; u < SK / 16; ++u) {
+        s[nt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (F16) {
+            s[nt][u] = pa_mfma(kr[u][ks], qh[nt][ks], s[nt][u]);
+            if constexpr (!SPLIT) s[nt][u] = pa_mfma(kr[u][ks], ql[nt][ks], s[nt][u]);
+          } else {
+            s[nt][u] = pa_mfma4(__builtin_bit_cast(f32x4, kr[u][ks]), __builtin_bit_cast(f32x4, qh[nt][ks]), s[nt][u]);
+          }
+        }
+      }
+    }
+    // the next step's keys take the registers of this one's; its values follow behind the value products
+    if (i + 1 < nsteps) {
+      place(i + 1, id1, (i + 1) & 1);
+      if (i + 2 < nsteps) id1 = page_load(i + 2);
+      load_k((i + 1) & 1);
     }
     u32x4 ph[NT], pl[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       if (nt > 0 && nt * 16 >= nr) break;
-      f32x4 s[SK / 16];
+      if constexpr (SPLIT) {
 #pragma unroll
-      for (int u = 0; u < SK / 16; ++u) {
-        s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          if constexpr (F16) {
-            s[u] = pa_mfma(st.k[u][ks], qh[nt][ks], s[u]);
-            if constexpr (!SPLIT) s[u] = pa_mfma(st.k[u][ks], ql[nt][ks], s[u]);
-          } else {
-            s[u] = pa_mfma4(__builtin_bit_cast(f32x4, st.k[u][ks]), __builtin_bit_cast(f32x4, qh[nt][ks]), s[u]);
-          }
-        }
-        if constexpr (SPLIT) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[u][e] += __shfl_xor(s[u][e], 8, kWave);
-        }
+          for (int e = 0; e < 4; ++e) s[nt][u][e] += pa_xor8(s[nt][u][e]);
       }
       float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[u][e] *= cf[nt];
-          if (tail) s[u][e] = base + u * 16 + grp * 4 + e < k1 ? s[u][e] : -INFINITY;
-          mx = fmaxf(mx, s[u][e]);
-        }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+        for (int e = 0; e < 4; ++e)
+          if (!tail || base + u * 16 + grp * 4 + e < k1) mx = fmaxf(mx, s[nt][u][e]);
+      mx = pa_max_groups(mx) * cf[nt];
       if (__any(mx > m[nt])) {
         const float mn = fmaxf(m[nt], mx);
         const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[nt] - mn);
@@ -339,27 +356,43 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
       }
       // (times 2^14 for fp16, so that small ones keep both halves; the sum has the same factor)
       const float mu = (m[nt] == -INFINITY ? 0.f : m[nt]) - (F16 ? 14.f : 0.f);
-      f16x8 hi, lo;
 #pragma unroll
       for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(s[u][e] - mu);
+          float p = __builtin_amdgcn_exp2f(fmaf(s[nt][u][e], cf[nt], -mu));
+          if (tail) p = base + u * 16 + grp * 4 + e < k1 ? p : 0.f;
           l[nt] += p;
-          s[u][e] = p;
-          if constexpr (F16) {
-            hi[u * 4 + e] = (_Float16)p;
-            lo[u * 4 + e] = (_Float16)(p - (float)hi[u * 4 + e]);
-          }
+          s[nt][u][e] = p;
         }
-      if constexpr (SPLIT) {
-        ph[nt] = col < 8 ? __builtin_bit_cast(u32x4, hi) : __builtin_bit_cast(u32x4, lo);
-      } else if constexpr (F16) {
-        ph[nt] = __builtin_bit_cast(u32x4, hi);
-        pl[nt] = __builtin_bit_cast(u32x4, lo);
+      if constexpr (F16) {
+        // first halves rounded towards zero (one instruction a pair), second halves to nearest: 2^-22 in all
+        u32x4 hi, lo;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p0 = s[nt][j >> 1][(j & 1) * 2], p1 = s[nt][j >> 1][(j & 1) * 2 + 1];
+          const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(p0, p1));
+          const f16x2 r = {(_Float16)fmaf((float)h[0], -1.f, p0), (_Float16)fmaf((float)h[1], -1.f, p1)};
+          hi[j] = __builtin_bit_cast(uint32_t, h);
+          lo[j] = __builtin_bit_cast(uint32_t, r);
+        }
+        if constexpr (SPLIT) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) ph[nt][j] = col < 8 ? hi[j] : lo[j];
+        } else {
+          ph[nt] = hi;
+          pl[nt] = lo;
+        }
       } else {
-        ph[nt] = __builtin_bit_cast(u32x4, s[0]);
+        ph[nt] = __builtin_bit_cast(u32x4, s[nt][0]);
       }
+    }
+    if (tail) {                                        // values behind the last row may be anything
+#pragma unroll
+      for (int k = 0; k < NK; ++k)
+        if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= k1)
+#pragma unroll
+          for (int mm = 0; mm < M; ++mm) vr[k][mm] = VT{};
     }
 #pragma unroll
     for (int mm = 0; mm < M; ++mm)
@@ -370,7 +403,7 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
           u32x4 v;
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            v[k] = __builtin_amdgcn_perm(st.v[2 * k + 1][mm][e >> 1], st.v[2 * k][mm][e >> 1],
+            v[k] = __builtin_amdgcn_perm(vr[2 * k + 1][mm][e >> 1], vr[2 * k][mm][e >> 1],
                                          e & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -381,7 +414,7 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
         } else {
           f32x4 v;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(st.v[k][mm][e]);
+          for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(vr[k][mm][e]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
             if (nt > 0 && nt * 16 >= nr) break;
@@ -389,31 +422,7 @@ __global__ void __launch_bounds__(kPaNT) k_paged_attn(PagedAttnArgs a) {
           }
         }
       }
-  };
-  // ---- stream: keys and values one step ahead, page indices two
-  auto ahead = [&](Step& st, int i, int buf) {         // issue the loads of step i
-    if (i >= nsteps) return;
-    place(i, id1, buf);
-    if (i + 1 < nsteps) id1 = page_load(i + 1);
-    load(st, buf);
-  };
-  if constexpr (Sh::DB) {
-    for (int i = 0; i < nsteps; i += 2) {
-      ahead(sb, i + 1, 1);
-      use(sa, i);
-      if (i + 1 >= nsteps) break;
-      ahead(sa, i + 2, 0);
-      use(sb, i + 1);
-    }
-  } else {
-    for (int i = 0; i < nsteps; ++i) {
-      load(sa, i & 1);
-      if (i + 1 < nsteps) {
-        place(i + 1, id1, (i + 1) & 1);
-        if (i + 2 < nsteps) id1 = page_load(i + 2);
-      }
-      use(sa, i);
-    }
+    if (i + 1 < nsteps) load_v((i + 1) & 1);
   }
 
   // ---- join the wavefronts: every one writes its sums (zeros where it had no step), then all threads add
