@@ -426,13 +426,15 @@ class Rotary:
     freq: torch.Tensor
     layout: int = DV_ROPE_HALF
     mscale: float = 1.0
+    _kept = _ck = None
 
     def c(self) -> CRotary:
-        key = (id(self.freq), self.layout, self.mscale)
-        if getattr(self, "_ck", None) != key:
+        # checked and built once per tensor (calls are on the hot path)
+        key = (self.layout, self.mscale)
+        if self.freq is not self._kept or self._ck != key:
             _tensor("Rotary.freq", self.freq, (torch.float64,), 1)
             self._cs = CRotary(2 * self.freq.shape[0], int(self.layout), _ptr(self.freq), float(self.mscale), 0)
-            self._ck, self._kept = key, self.freq     # (kept: no other tensor gets its id)
+            self._ck, self._kept = key, self.freq
         return self._cs
 
 
@@ -443,11 +445,12 @@ class PagedKV:
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
         self.K, self.V, self.table = K, V, table
+        self._kept = (None, None, None)
 
     def c(self) -> CPagedKV:
         # checked and built once per set of tensors (calls are on the hot path)
-        key = (id(self.K), id(self.V), id(self.table))
-        if getattr(self, "_ck", None) != key:
+        kept = self._kept
+        if self.K is not kept[0] or self.V is not kept[1] or self.table is not kept[2]:
             for nm in ("K", "V"):
                 t = getattr(self, nm)
                 if not isinstance(t, torch.Tensor):
@@ -468,7 +471,7 @@ class PagedKV:
             _gpu("PagedKV", self.K, self.V, self.table)
             self._cs = CPagedKV(H, dh, page, n_pages, self.table.shape[0], self.table.shape[1], _wtype(self.K), 0,
                                 *strides, _ptr(self.K), _ptr(self.V), _ptr(self.table))
-            self._ck, self._kept = key, (self.K, self.V, self.table)   # (kept: no other tensor gets their ids)
+            self._kept = (self.K, self.V, self.table)
         return self._cs
 
 
@@ -737,30 +740,53 @@ def _tokens(name, x, heads=None, dh=None, rows=None, dtype=None):
     return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
 
 
-def _fits_i32(t, shape) -> bool:
-    return type(t) is torch.Tensor and t.dtype is torch.int32 and t.shape == shape and t.is_cuda and t.is_contiguous()
-
-
 def _index(name, t, shape, optional=False):
-    if not ((t is None and optional) or _fits_i32(t, shape)):
-        _tensor(name, t, _I32, len(shape), shape, optional=optional)
+    _tensor(name, t, _I32, len(shape), shape, optional=optional)
+
+
+_WTYPE = {torch.float16: DV_F16, torch.float32: DV_F32}
+_current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on(t, dtype, dev) -> bool:
+    """Whether t is a plain contiguous tensor of this dtype on device number dev (the usual case; what is not goes
+    through the full checks, which accept or name it)."""
+    return type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == dev and t.is_contiguous()
+
+
+def _stride_on(t, dtype, shape, dev):
+    """The token stride of a plain [tokens][heads][dh] tensor on device number dev (0: not the usual case)."""
+    if type(t) is not torch.Tensor or t.dtype is not dtype or t.shape != shape or t.get_device() != dev:
+        return 0
+    s0, s1, s2 = t.stride()
+    row = shape[1] * shape[2]
+    return s0 if s2 == 1 and s1 == shape[2] and s0 >= row else 0
 
 
 def dv_rope(rotary: Rotary, x, pos, inverse=False, out=None, stream=None):
     """x [T][H][dh] (fp16 or fp32) rotated at positions pos [T]; inverse: by the negative angles (the
     gradient's direction). out=x rotates in place."""
-    lib = load()
+    lib = _lib or load()
     cr = rotary.c()
-    ldx = _tokens("x", x)
+    dev = _current()
+    ldx = _stride_on(x, x.dtype, x.shape, dev) if type(x) is torch.Tensor and x.dim() == 3 and x.dtype in _STORE else 0
+    if not (ldx and _on(pos, torch.int32, dev) and pos.dim() == 1 and pos.shape[0] == x.shape[0]
+            and rotary.freq.get_device() == dev):
+        ldx = _tokens("x", x)
+        _index("pos", pos, (x.shape[0],))
+        _here(x, pos, rotary.freq)
     T, H, dh = x.shape
-    _index("pos", pos, (T,))
     mine = out is None
     if mine:
         out = torch.empty((T, H, dh), dtype=x.dtype, device=x.device)
-    ldo = ldx if out is x else _tokens("out", out, H, dh, T, x.dtype)
-    _here(x, pos, out, rotary.freq)
-    _check("dv_rope", lib.dv_rope(ctypes.byref(cr), _ptr(x), ldx, _wtype(x), T, H, dh, _ptr(pos), _ptr(out), ldo,
-                                  DV_ROPE_INVERSE if inverse else 0, _stream(stream)))
+    ldo = ldx if out is x else _stride_on(out, x.dtype, x.shape, dev)
+    if not ldo:
+        ldo = _tokens("out", out, H, dh, T, x.dtype)
+        _here(out)
+    st = lib.dv_rope(ctypes.byref(cr), x.data_ptr(), ldx, _WTYPE[x.dtype], T, H, dh, pos.data_ptr(), out.data_ptr(), ldo,
+                     DV_ROPE_INVERSE if inverse else 0, _stream(stream))
+    if st:
+        _check("dv_rope", st)
     if mine:
         _used_on(stream, out)
     return out
@@ -771,33 +797,53 @@ def dv_paged_append(kv: PagedKV, k, v, pos, seq=None, rotary: Optional[Rotary] =
     """Keys and values k, v [T][H][dh] of new tokens into their rows pos [T] of sequences seq [T] (None: token t is
     of sequence t), keys rotated if `rotary` is given; tokens with pos < 0 are left out. heads [T][n]: only
     those key/value heads. q [T][Hq][dh]: rotated into q_out (q_out=q: in place), which is returned."""
-    lib = load()
+    lib = _lib or load()
     ck = kv.c()
     cr = rotary.c() if rotary is not None else None
-    ldk = _tokens("k", k, ck.H, ck.dh)
-    T = k.shape[0]
-    ldv = _tokens("v", v, ck.H, ck.dh, T, k.dtype)
-    _index("pos", pos, (T,))
-    _index("seq", seq, (T,), optional=True)
-    n_heads = 0
+    dev = _current()
+    dt = k.dtype if type(k) is torch.Tensor else None
+    ldk = ldv = 0
+    if dt in _STORE and k.dim() == 3:
+        shape = (k.shape[0], ck.H, ck.dh)
+        ldk, ldv = _stride_on(k, dt, shape, dev), _stride_on(v, dt, shape, dev)
+    if not (ldk and ldv and _on(pos, torch.int32, dev) and pos.shape == shape[:1] and kv.K.get_device() == dev
+            and (seq is None or (_on(seq, torch.int32, dev) and seq.shape == shape[:1]))
+            and (rotary is None or rotary.freq.get_device() == dev)):
+        ldk = _tokens("k", k, ck.H, ck.dh)
+        T = k.shape[0]
+        ldv = _tokens("v", v, ck.H, ck.dh, T, k.dtype)
+        _index("pos", pos, (T,))
+        _index("seq", seq, (T,), optional=True)
+        _here(k, v, pos, seq, kv.K, kv.V, kv.table, rotary.freq if rotary is not None else None)
+    T, dt = k.shape[0], k.dtype
+    n_heads = ldq = ldqo = Hq = 0
     if heads is not None:
-        _index("heads", heads, (T, None) if not isinstance(heads, torch.Tensor) or heads.dim() != 2 else (T, heads.shape[1]))
+        if not (_on(heads, torch.int32, dev) and heads.dim() == 2 and heads.shape[0] == T):
+            _index("heads", heads, (T, None))
+            _here(heads)
         n_heads = heads.shape[1]
-    ldq = ldqo = Hq = 0
     mine = q is not None and q_out is None
     if q is not None:
-        ldq = _tokens("q", q, None, ck.dh, T, k.dtype)
+        ldq = _stride_on(q, dt, (T, q.shape[1], ck.dh), dev) if type(q) is torch.Tensor and q.dim() == 3 else 0
+        if not ldq:
+            ldq = _tokens("q", q, None, ck.dh, T, dt)
+            _here(q)
         Hq = q.shape[1]
         if mine:
             # (rows of idle tokens are not written)
-            q_out = torch.zeros((T, Hq, ck.dh), dtype=q.dtype, device=q.device)
-        ldqo = ldq if q_out is q else _tokens("q_out", q_out, Hq, ck.dh, T, k.dtype)
+            q_out = torch.zeros((T, Hq, ck.dh), dtype=dt, device=q.device)
+        ldqo = ldq if q_out is q else _stride_on(q_out, dt, (T, Hq, ck.dh), dev)
+        if not ldqo:
+            ldqo = _tokens("q_out", q_out, Hq, ck.dh, T, dt)
+            _here(q_out)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    _here(k, v, pos, seq, heads, q, q_out, kv.K, kv.V, kv.table, rotary.freq if rotary is not None else None)
-    _check("dv_paged_append", lib.dv_paged_append(
-        ctypes.byref(ck), ctypes.byref(cr) if cr is not None else None, _ptr(k), ldk, _ptr(v), ldv, _wtype(k), T, _ptr(seq),
-        _ptr(pos), _ptr(heads), n_heads, _ptr(q), ldq, Hq, _ptr(q_out), ldqo, _stream(stream)))
+    st = lib.dv_paged_append(
+        ctypes.byref(ck), None if cr is None else ctypes.byref(cr), k.data_ptr(), ldk, v.data_ptr(), ldv, _WTYPE[dt], T,
+        None if seq is None else seq.data_ptr(), pos.data_ptr(), None if heads is None else heads.data_ptr(), n_heads,
+        None if q is None else q.data_ptr(), ldq, Hq, None if q is None else q_out.data_ptr(), ldqo, _stream(stream))
+    if st:
+        _check("dv_paged_append", st)
     if mine:
         _used_on(stream, q_out)
     return q_out
@@ -815,15 +861,20 @@ def dv_paged_attn(kv: PagedKV, q, pos, max_len, scale, seq=None, heads=None, q_h
     q_heads (= n unless given) query heads, or each token's set heads [T][n] of them. shared_pages: leading pages that
     all sequences share, attended once for the batch. Returns out [T][n][dh], or (out, lse) if lse [T][n]
     (the log-sum-exp of the logits) is given."""
-    lib = load()
+    lib = _lib or load()
     ck = kv.c()
     dh = ck.dh
-    if not (type(q) is torch.Tensor and q.dim() == 3 and _fits(q, torch.float32, (q.shape[0], q.shape[1], dh))):
+    dev = _current()
+    if not (_on(q, torch.float32, dev) and q.dim() == 3 and q.shape[2] == dh and kv.K.get_device() == dev):
         _tensor("q", q, _F32, 3, (None, None, dh))
-    T, n = q.shape[0], q.shape[1]
-    _index("pos", pos, (T,))
-    _index("seq", seq, (T,), optional=True)
-    _index("heads", heads, (T, n), optional=True)
+        _here(q, kv.K, kv.V, kv.table)
+    T, n, _ = q.shape
+    if not (_on(pos, torch.int32, dev) and pos.shape == (T,) and (seq is None or (_on(seq, torch.int32, dev) and seq.shape == (T,)))
+            and (heads is None or (_on(heads, torch.int32, dev) and heads.shape == (T, n)))):
+        _index("pos", pos, (T,))
+        _index("seq", seq, (T,), optional=True)
+        _index("heads", heads, (T, n), optional=True)
+        _here(pos, seq, heads)
     if q_heads is None:
         q_heads = n if heads is None else ck.H
     if heads is None and q_heads != n:
@@ -832,19 +883,27 @@ def dv_paged_attn(kv: PagedKV, q, pos, max_len, scale, seq=None, heads=None, q_h
     if out is None:
         out = torch.empty_like(q)
         mine.append(out)
-    elif not _fits(out, torch.float32, q.shape):
+    elif not (_on(out, torch.float32, dev) and out.shape == q.shape):
         _tensor("out", out, _F32, 3, tuple(q.shape))
-    if lse is not None and not _fits(lse, torch.float32, (T, n)):
+        _here(out)
+    if lse is not None and not (_on(lse, torch.float32, dev) and lse.shape == (T, n)):
         _tensor("lse", lse, _F32, 2, (T, n))
+        _here(lse)
     if ws is None:
         ws = _workspace(lib.dv_paged_attn_workspace_bytes(ctypes.byref(ck), T, q_heads, 0 if heads is None else n,
                                                           max_len, shared_pages), q.device)
         mine.append(ws)
-    _here(q, pos, seq, heads, out, lse, ws, kv.K, kv.V, kv.table)
-    _check("dv_paged_attn", lib.dv_paged_attn(
-        ctypes.byref(ck), _ptr(q), T, q_heads, _ptr(heads), 0 if heads is None else n, _ptr(seq), _ptr(pos), max_len,
-        shared_pages, scale, _ptr(out), _ptr(lse), *_wsarg(ws), flags, _stream(stream)))
-    _used_on(stream, *mine)
+    elif not (_on(ws, torch.uint8, dev) and ws.dim() == 1):
+        _tensor("ws", ws, (torch.uint8,), 1)
+        _here(ws)
+    st = lib.dv_paged_attn(
+        ctypes.byref(ck), q.data_ptr(), T, q_heads, None if heads is None else heads.data_ptr(), 0 if heads is None else n,
+        None if seq is None else seq.data_ptr(), pos.data_ptr(), max_len, shared_pages, scale, out.data_ptr(),
+        None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), flags, _stream(stream))
+    if st:
+        _check("dv_paged_attn", st)
+    if mine and stream is not None:
+        _used_on(stream, *mine)
     return out if lse is None else (out, lse)
 
 

@@ -582,7 +582,7 @@ hipError_t launch_paged_combine(const PagedAttnArgs& a, hipStream_t st) {
 static int pa_variant(int ktype, int dh, int most) {
   const bool f16 = ktype == DV_F16;
   if (most <= (f16 ? 8 : 16)) return 0;
-  return most <= 32 || dh > 128 ? 2 : 4;
+  return 2;
 }
 static int pa_rows(int ktype, int qt) { return qt == 0 ? (ktype == DV_F16 ? 8 : 16) : 16 * qt; }
 
