@@ -413,7 +413,7 @@ typedef struct dv_paged_kv {
   int32_t H, dh;              /* key/value heads, head width (dh elements a multiple of 16 bytes, dh <= 256) */
   int32_t page;               /* rows of a page (>= 1; any number) */
   int32_t n_pages;            /* pages of the pool */
-  int32_t n_seq, max_pages;   /* the table's rows and their length; max_pages * page < 2^31 */
+  int32_t n_seq, max_pages;   /* the table's rows and their length; max_pages * page < 2^31 - 4096 */
   int32_t ktype;              /* dv_dtype of K and V: DV_F16 or DV_F32 */
   int32_t reserved;           /* must be 0 */
   int64_t page_stride, head_stride, row_stride;

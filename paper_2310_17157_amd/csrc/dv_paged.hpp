@@ -40,23 +40,29 @@ struct RopeArgs {
 };
 hipError_t launch_rope(int xtype, int ktype, int layout, const RopeArgs& a, hipStream_t st);
 
-// Attention of T tokens over the pages. Partials of a row (token, place j): slots [0, SP) from the
-// shared rows, SP + s from part s of its own rows: ml[row][slot] = (max, sum), o[row][slot][dh].
+// Attention of T tokens over the pages. Workgroups: first the shared rows' (key head, part, tile of query rows), then
+// items x units of the tokens' own rows: an item is a run of a token's (a group's) rows, a unit a key head's tile of
+// query rows, or a place of a head set. Partials: (max, sum) and a value sum each, of the shared rows by [row][part], of
+// own rows by [workgroup][row of it].
 struct PagedAttnArgs {
   Pages g;
   const float* q; const int32_t* heads; const int32_t* seq; const int32_t* pos;
   int T, n, G;                      // tokens, query heads a token, query heads a key head
   int max_len;
   float scale;                      // times log2(e)
+  int RT, U, row_tiles, group_tiles;   // query rows of a workgroup; units; tiles of a key head's shared and own rows
   int P, SP, CP;                    // shared rows, parts of them, rows of a part
-  int S, cmin;                      // parts of a token's own rows, least rows of a part
-  int row_tiles, group_tiles;       // row tiles of a key head's shared work, of a token's own
-  int n_shared;                     // workgroups of the shared work (first in the grid)
-  float* ml; float* o; int slots;   // partials (slots == 1 and P == 0: written out directly)
+  int n_shared;                     // workgroups of the shared rows
+  int target;                       // workgroups that the own rows are cut for (0: an item is a token)
+  int items, cmin;                  // items at most, least rows of one
+  int gmax, RW;                     // tokens of a group at most, rows that a workgroup keeps partials of
+  bool direct;                      // one part each: written out by the attention itself
+  float *sml, *so, *oml, *oo;       // partials of shared and own rows
+  int4* meta;                       // [T] (target > 0) where a token's own partials are
   float* out; int ldo;              // row r at out + r ldo; ldo = dh + 2: (0, 1) before its dh values
   float* lse;
 };
-// The parts that a launch is cut into (P, SP, CP, S, cmin, row and group tiles, slots) for these sizes.
+// How a launch is cut (all of the second block) for the sizes in g, n, G, T, max_len, P, with or without heads and seq.
 void plan_paged_attn(PagedAttnArgs* a, int ktype);
 hipError_t launch_paged_attn(int ktype, const PagedAttnArgs& a, hipStream_t st);
 hipError_t launch_paged_combine(const PagedAttnArgs& a, hipStream_t st);

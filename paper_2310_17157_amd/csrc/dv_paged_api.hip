@@ -37,7 +37,7 @@ dv_status check_paged(const dv_paged_kv* kv) {
     return DV_ERR_SHAPE;
   if ((kv->dh * elem_bytes(kv->ktype)) % 16 != 0) return DV_ERR_ALIGN;
   if (!aligned16(kv->K) || !aligned16(kv->V) || !aligned_to(kv->table, 4)) return DV_ERR_ALIGN;
-  if (kv->dh > 256 || (int64_t)kv->max_pages * kv->page > INT32_MAX) return DV_ERR_UNSUPPORTED;
+  if (kv->dh > 256 || (int64_t)kv->max_pages * kv->page > INT32_MAX - 4096) return DV_ERR_UNSUPPORTED;
   return check_strides(kv);
 }
 
@@ -76,23 +76,27 @@ void set_rotary(RopeArgs* a, const dv_rotary* r) {
 constexpr int64_t kMaxPagedRows = 1 << 22;
 constexpr int kMaxUnionHeads = 131072;               // heads of a batch's union (dv_sparse_attn's limit)
 
-// The launch of T tokens with n query heads each (heads: non-NULL for head sets) and its partials in w.
-PagedAttnArgs attn_args(const dv_paged_kv* kv, int T, int Hq, const int32_t* heads, int n, int max_len, int shared_pages,
-                        Workspace& w) {
+// The launch of T tokens with n query heads each (heads: non-NULL for head sets; seq: NULL or not) and its partials in w.
+PagedAttnArgs attn_args(const dv_paged_kv* kv, int T, int Hq, const int32_t* heads, int n, const int32_t* seq, int max_len,
+                        int shared_pages, Workspace& w) {
   PagedAttnArgs a{};
   a.g = pages_of(kv);
-  a.T = T; a.n = n; a.G = Hq / kv->H; a.heads = heads; a.max_len = max_len; a.P = shared_pages * kv->page;
+  a.T = T; a.n = n; a.G = Hq / kv->H; a.heads = heads; a.seq = seq; a.max_len = max_len; a.P = shared_pages * kv->page;
   plan_paged_attn(&a, kv->ktype);
-  if (a.slots > 1 || a.P > 0) {
-    a.ml = w.take<float>((size_t)T * n * a.slots * 2 * sizeof(float));
-    a.o = w.take<float>((size_t)T * n * a.slots * kv->dh * sizeof(float));
+  if (!a.direct) {
+    const size_t shared = (size_t)T * n * a.SP, own = (size_t)a.items * a.U * a.RW;
+    a.sml = w.take<float>(shared * 2 * sizeof(float));
+    a.so = w.take<float>(shared * kv->dh * sizeof(float));
+    a.oml = w.take<float>(own * 2 * sizeof(float));
+    a.oo = w.take<float>(own * kv->dh * sizeof(float));
+    a.meta = w.take<int4>((size_t)T * sizeof(int4));
   }
   return a;
 }
 
 dv_status enqueue_paged_attn(const PagedAttnArgs& a, int ktype, hipStream_t st) {
   DV_LAUNCH("paged_attn", st, launch_paged_attn(ktype, a, st));
-  if (a.slots > 1 || a.P > 0) DV_LAUNCH("paged_combine", st, launch_paged_combine(a, st));
+  if (!a.direct) DV_LAUNCH("paged_combine", st, launch_paged_combine(a, st));
   return DV_OK;
 }
 
@@ -117,7 +121,7 @@ size_t paged_step_ws(const dv_paged_kv* kv, int B, int n_heads, int max_len, int
   if (n_heads == 0) return 0;
   Workspace w(nullptr);
   const int32_t some = 0;
-  (void)attn_args(kv, B, kv->H, &some, n_heads, max_len, shared_pages, w);
+  (void)attn_args(kv, B, kv->H, &some, n_heads, &some, max_len, shared_pages, w);
   return w.off;
 }
 
@@ -131,8 +135,8 @@ dv_status paged_step(const PagedStep& p, int B, const int32_t* heads, int n_head
   r.g = pages_of(p.kv);
   DV_LAUNCH("append", st, launch_rope(DV_F32, p.kv->ktype, p.r != nullptr ? p.r->layout : DV_ROPE_HALF, r, st));
   Workspace w(ws);
-  PagedAttnArgs a = attn_args(p.kv, B, p.kv->H, heads, n_heads, p.max_len, p.shared_pages, w);
-  a.q = q; a.seq = p.seq; a.pos = p.pos; a.scale = p.scale * (float)M_LOG2E; a.out = part; a.ldo = dh + 2;
+  PagedAttnArgs a = attn_args(p.kv, B, p.kv->H, heads, n_heads, p.seq, p.max_len, p.shared_pages, w);
+  a.q = q; a.pos = p.pos; a.scale = p.scale * (float)M_LOG2E; a.out = part; a.ldo = dh + 2;
   return enqueue_paged_attn(a, p.kv->ktype, st);
 }
 
@@ -232,10 +236,14 @@ extern "C" size_t dv_paged_attn_workspace_bytes(const dv_paged_kv* kv, int32_t T
     return 0;
   const int n = n_heads > 0 ? n_heads : Hq;
   if ((int64_t)T * n > kMaxPagedRows || (int64_t)T * kv->H > kMaxPagedRows) return 0;
-  Workspace w(nullptr);
-  w.take<int32_t>(sizeof(int32_t));
-  if (T > 0) (void)attn_args(kv, T, Hq, n_heads > 0 ? &kSomeHeads : nullptr, n, max_len, shared_pages, w);
-  return w.off;
+  size_t most = 0;
+  for (const int32_t* seq : {static_cast<const int32_t*>(nullptr), &kSomeHeads}) {   // (groups of drafts need seq)
+    Workspace w(nullptr);
+    w.take<int32_t>(sizeof(int32_t));
+    if (T > 0) (void)attn_args(kv, T, Hq, n_heads > 0 ? &kSomeHeads : nullptr, n, seq, max_len, shared_pages, w);
+    most = std::max(most, w.off);
+  }
+  return most;
 }
 
 extern "C" dv_status dv_paged_attn(const dv_paged_kv* kv, const float* q, int32_t T, int32_t Hq, const int32_t* heads,
@@ -257,14 +265,14 @@ extern "C" dv_status dv_paged_attn(const dv_paged_kv* kv, const float* q, int32_
   if (!ws_ok(ws)) return DV_ERR_WORKSPACE;
   Workspace w(ws);
   int32_t* flag = w.take<int32_t>(sizeof(int32_t));
-  PagedAttnArgs a = attn_args(kv, T, Hq, heads, n, max_len, shared_pages, w);
+  PagedAttnArgs a = attn_args(kv, T, Hq, heads, n, seq, max_len, shared_pages, w);
   if (w.off > ws_bytes) return DV_ERR_WORKSPACE;
   hipStream_t hs = static_cast<hipStream_t>(stream);
   if (flags & DV_VALIDATE) {
     if (heads != nullptr && (st = validate_sets_sync(heads, T, n, Hq, flag, hs)) != DV_OK) return st;
     if ((st = validate_paged_sync(kv, seq, pos, T, max_len, shared_pages, flag, hs)) != DV_OK) return st;
   }
-  a.q = q; a.seq = seq; a.pos = pos; a.scale = scale * (float)M_LOG2E; a.out = out; a.ldo = kv->dh; a.lse = lse;
+  a.q = q; a.pos = pos; a.scale = scale * (float)M_LOG2E; a.out = out; a.ldo = kv->dh; a.lse = lse;
   return enqueue_paged_attn(a, kv->ktype, hs);
 }
 

@@ -26,6 +26,7 @@
 // from one set of registers, and more wavefronts fit than with two sets.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "dv_paged.hpp"
@@ -37,22 +38,99 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kPaNW = 4, kPaNT = 64 * kPaNW;
 constexpr float kPaLn2 = 0.693147180559945309f;
-constexpr int kPaMaxSlots = 64;      // parts of the shared rows, and of a token's own, at most
+constexpr int kPaMaxParts = 64;      // parts of the shared rows, and of a group's own, at most
 
-// What a token attends: len rows in all, of which its own start at `start` (behind the shared rows, if it
-// attends all of those), in `parts` parts of `chunk` rows.
-struct Own { int len, start, chunk, parts; };
-__device__ __forceinline__ Own own_rows(const PagedAttnArgs& a, int t) {
-  Own o;
-  o.len = min(max(a.pos[t], -1), a.max_len - 1) + 1;
-  o.start = a.P > 0 && o.len >= a.P ? a.P : 0;
-  const int n = o.len - o.start;
-  o.chunk = max(a.cmin, ((n + a.S - 1) / a.S + 127) & ~127);
-  o.parts = (n + o.chunk - 1) / o.chunk;
-  return o;
+// Rows that token t attends, and how many of them are shared ones (all of those, or none: a token that attends fewer
+// takes what it attends by itself).
+__device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int t) { return min(max(a.pos[t], -1), a.max_len - 1) + 1; }
+__device__ __forceinline__ int pa_start(const PagedAttnArgs& a, int len) { return a.P > 0 && len >= a.P ? a.P : 0; }
+
+// Tokens next to each other that share a sequence (drafts) are a group, whose own rows are read once: up to gmax of
+// them (aligned), at ascending positions not far apart. True for the first token of a group.
+constexpr int kPaGroupSpan = 64;
+__device__ __forceinline__ bool pa_leads(const PagedAttnArgs& a, int t) {
+  if (a.gmax == 1 || t % a.gmax == 0) return true;
+  const int p = a.pos[t], b = a.pos[t - 1];
+  return a.seq[t] != a.seq[t - 1] || b < 0 || p < b || p - b > kPaGroupSpan ||
+         pa_start(a, pa_len(a, t)) != pa_start(a, pa_len(a, t - 1));
+}
+// A group's own rows, at its last token (0 at the others).
+__device__ __forceinline__ int pa_own(const PagedAttnArgs& a, int t) {
+  if (t >= a.T || (t + 1 < a.T && !pa_leads(a, t + 1))) return 0;
+  const int len = pa_len(a, t);
+  return len - pa_start(a, len);
 }
 
-template <typename KT, int DH, int QT>
+// How the groups' own rows are cut: runs of `chunk` rows, chosen from what the batch attends now (every wavefront
+// computes the same), so that a.target workgroups share them evenly. Items are numbered: the whole
+// runs of all groups, then the groups' rests (the short ones last, where the last workgroups are waited for).
+struct PaCut { int chunk, whole; };
+__device__ __forceinline__ int pa_wave_incl(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int n = __shfl_up(v, o, kWave);
+    if (lane >= o) v += n;
+  }
+  return v;
+}
+__device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, int U, int lane) {
+  float rows = 0.f;
+  int most = 0;
+  for (int b = 0; b < a.T; b += kWave) {
+    const int n = pa_own(a, b + lane);
+    rows += (float)n;
+    most = max(most, n);
+  }
+  rows = wave_sum(rows);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
+  // (a little more than the even share: the rows' sum is rounded)
+  const float even = fminf(rows * 1.0001f * (float)U / (float)a.target + 1.f, 1e9f);
+  PaCut c;
+  c.chunk = max(max(a.cmin, (int)even), most / (kPaMaxParts - 1) + 1);
+  c.chunk = (c.chunk + 127) & ~127;
+  c.whole = 0;
+  for (int b = 0; b < a.T; b += kWave) c.whole += pa_own(a, b + lane) / c.chunk;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) c.whole += __shfl_xor(c.whole, o, kWave);
+  return c;
+}
+// The group (its last token) and run of an item; -1: there is no such item.
+__device__ __forceinline__ int pa_find(const PagedAttnArgs& a, const PaCut& c, int item, int lane, int* run) {
+  int seen = item < c.whole ? 0 : c.whole;
+  for (int b = 0; b < a.T; b += kWave) {
+    const int n = pa_own(a, b + lane), w = n / c.chunk;
+    const int mine = item < c.whole ? w : (n - w * c.chunk > 0 ? 1 : 0);
+    const int incl = seen + pa_wave_incl(mine, lane);
+    const unsigned long long hit = __ballot(item < incl && item >= incl - mine);
+    if (hit != 0) {
+      const int l = __builtin_ctzll(hit);
+      *run = item < c.whole ? item - (__shfl(incl, l, kWave) - __shfl(mine, l, kWave)) : __shfl(w, l, kWave);
+      return b + l;
+    }
+    seen = __shfl(incl, kWave - 1, kWave);
+  }
+  return -1;
+}
+// For the join: per token its group's first whole run, their number, the rest's item or -1, and the group's first token.
+__device__ __forceinline__ void pa_write_meta(const PagedAttnArgs& a, const PaCut& c, int lane) {
+  int whole = 0, rest = c.whole;
+  for (int b = 0; b < a.T; b += kWave) {
+    const int t = b + lane;
+    const int n = pa_own(a, t), w = n / c.chunk, r = n - w * c.chunk > 0 ? 1 : 0;
+    const int iw = whole + pa_wave_incl(w, lane), ir = rest + pa_wave_incl(r, lane);
+    if (t < a.T && (t + 1 == a.T || pa_leads(a, t + 1))) {
+      int lead = t;
+      while (!pa_leads(a, lead)) --lead;
+      for (int m = lead; m <= t; ++m) a.meta[m] = int4{iw - w, w, r ? ir - 1 : -1, lead};
+    }
+    whole = __shfl(iw, kWave - 1, kWave);
+    rest = __shfl(ir, kWave - 1, kWave);
+  }
+}
+
+// FULL: heads are DH elements wide (else up to DH, pieces past a row's end read its last bytes again).
+template <typename KT, int DH, int QT, bool FULL>
 struct PaShape {
   static constexpr bool F16 = std::is_same<KT, _Float16>::value;
   static constexpr bool SPLIT = F16 && QT == 0;       // both halves of a query in one tile
@@ -63,7 +141,11 @@ struct PaShape {
   static constexpr int CH = F16 ? (DH == 64 ? 4 : 8) : 4;   // elements of a lane's chunk of a value
   static constexpr int M = DH / (16 * CH);            // chunks of a lane
   static constexpr int DHP = DH + 4;                  // LDS row of the join
-  static constexpr int WAVES = DH == 64 ? (QT == 0 ? 4 : QT == 2 ? 3 : 2) : DH == 128 ? (QT == 0 ? 3 : QT == 2 ? 2 : 1) : 1;
+  // wavefronts a SIMD: as many as leave each its registers (a register spilled inside the loop would wait for all
+  // loads before it, the next step's among them)
+  static constexpr int WAVES = DH == 64 ? (QT == 0 ? 4 : 2) : DH == 128 ? (QT == 0 && FULL ? 3 : 2) : 1;
+  // queries in LDS (the space of the join) instead of registers: their second halves, or all
+  static constexpr bool QLO = F16 && QT == 2 && DH >= 128, QALL = QT == 2 && DH == 256;
   static constexpr size_t lds() { return (size_t)kPaNW * RT * (DHP + 2) * sizeof(float); }
 };
 
@@ -96,9 +178,9 @@ __device__ __forceinline__ f32x4 pa_mfma4(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-template <typename KT, int DH, int QT>
-__global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_attn(PagedAttnArgs a) {
-  using Sh = PaShape<KT, DH, QT>;
+template <typename KT, int DH, int QT, bool FULL>
+__global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_paged_attn(PagedAttnArgs a) {
+  using Sh = PaShape<KT, DH, QT, FULL>;
   constexpr bool F16 = Sh::F16, SPLIT = Sh::SPLIT;
   constexpr int NT = Sh::NT, RT = Sh::RT, SK = Sh::SK, KS = Sh::KS, CH = Sh::CH, M = Sh::M, DHP = Sh::DHP;
   constexpr int NK = F16 ? 8 : 4;                      // cache rows of a lane in the value product
@@ -107,12 +189,14 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
   __shared__ int red[kPaNW + 1];
   __shared__ int64_t offs[kPaNW][2][SK];
   extern __shared__ float smem[];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;   // (a scalar: so are the steps)
   const int col = lane & 15, grp = lane >> 4;
 
-  // ---- the unit: query rows (rows[0..nr): index t n + j, or -1), key head, cache rows [k0, k1), table row, slot
-  int h, tile, k0, k1, slot, c0 = 0, c1 = 0;           // [c0, c1): candidates of head sets to look through
-  bool shared = (int)blockIdx.x < a.n_shared;
+  // ---- the unit: query rows (rows[0..nr): index t n + j, or -1), key head, cache rows [k0, k1), place of its partials
+  int h, tile, k0, k1, c0 = 0, c1 = 0;                 // [c0, c1): candidates of head sets to look through
+  int group = 1, lead = 0;                             // tokens of the unit (own rows), the first
+  int64_t place0;                                      // partials: row index * SP + part, or workgroup * RW + row
+  const bool shared = (int)blockIdx.x < a.n_shared;
   if (shared) {
     // the row tiles of a part 8 workgroups apart: on one XCD, whose L2 then holds the part's keys and values
     const int b = blockIdx.x, x = b & 7, y = b >> 3;
@@ -120,8 +204,9 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
     tile = y % a.row_tiles;
     if (u >= a.g.H * a.SP) return;
     h = u / a.SP;
-    slot = u - h * a.SP;
-    k0 = slot * a.CP;
+    const int part = u - h * a.SP;
+    place0 = part;
+    k0 = part * a.CP;
     k1 = min(k0 + a.CP, a.P);
     if (a.heads != nullptr) c1 = a.T * a.n;
     if (a.heads == nullptr && tid < RT) {
@@ -129,34 +214,53 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
       int idx = -1;
       if (c < a.T * a.G) {
         const int t = c / a.G;
-        if (min(a.pos[t], a.max_len - 1) + 1 >= a.P) idx = t * a.n + h * a.G + (c - t * a.G);
+        if (pa_len(a, t) >= a.P) idx = t * a.n + h * a.G + (c - t * a.G);
       }
       rows[tid] = idx;
     }
   } else {
-    int w = (int)blockIdx.x - a.n_shared;
-    const int s = w % a.S;
-    w /= a.S;
-    tile = w % a.group_tiles;
-    w /= a.group_tiles;
-    const bool single = a.heads != nullptr && a.G == 1;   // one row: the unit is (token, place in its set)
-    const int t = w / (single ? a.n : a.g.H), x = w - t * (single ? a.n : a.g.H);
-    const Own o = own_rows(a, t);
-    slot = a.SP + s;
-    h = x;
-    if (single) {
-      h = min(max(a.heads[(int64_t)t * a.n + x], 0), a.g.H - 1);
-      if (tid < RT) rows[tid] = tid == 0 ? t * a.n + x : -1;
-    } else if (a.heads == nullptr) {
-      if (tid < RT) rows[tid] = tile * RT + tid < a.G ? t * a.n + h * a.G + tile * RT + tid : -1;
-    } else {
-      c0 = t * a.n;
-      c1 = c0 + a.n;
+    const int id = (int)blockIdx.x - a.n_shared;
+    const int item = id / a.U, u = id - item * a.U;
+    int t = item, run = 0, chunk = INT32_MAX;
+    if (a.target > 0) {
+      const PaCut cut = pa_cut(a, a.U, lane);
+      if (id == 0 && wave == 0) pa_write_meta(a, cut, lane);
+      t = pa_find(a, cut, item, lane, &run);
+      if (t < 0) return;
+      chunk = cut.chunk;
+    } else if (t + 1 < a.T && !pa_leads(a, t + 1)) {
+      return;                                          // (its group's last token takes it)
     }
-    k0 = o.start + s * o.chunk;
-    k1 = min(k0 + o.chunk, o.len);
-    // a part that the token does not have; a token without rows is still to be written by its only part
-    if (k0 >= k1 && (a.slots > 1 || a.P > 0)) return;
+    lead = t;
+    if (a.gmax > 1) {                                  // lane k: does token t - k lead?
+      const bool first = lane < a.gmax && lane <= t && pa_leads(a, t - lane);
+      lead = t - __builtin_ctzll(__ballot(first));
+    }
+    group = t - lead + 1;
+    const bool single = a.heads != nullptr && a.G == 1;   // one row: the unit is (token, place in its set)
+    if (single) {
+      tile = 0;
+      h = min(max(a.heads[(int64_t)t * a.n + u], 0), a.g.H - 1);
+      if (tid < RT) rows[tid] = tid == 0 ? t * a.n + u : -1;
+    } else {
+      h = u / a.group_tiles;
+      tile = u - h * a.group_tiles;
+      if (a.heads == nullptr) {
+        if (tid < RT) {
+          const int r = tile * RT + tid, g = r / a.G;    // (group > 1: one tile)
+          rows[tid] = r < group * a.G ? (lead + g) * a.n + h * a.G + (r - g * a.G) : -1;
+        }
+      } else {
+        c0 = t * a.n;
+        c1 = c0 + a.n;
+      }
+    }
+    const int len = pa_len(a, t);
+    k0 = pa_start(a, len) + run * (run > 0 ? chunk : 0);
+    k1 = chunk < len - k0 ? k0 + chunk : len;
+    place0 = (int64_t)id * a.RW;
+    // nothing of its own to attend: the join does without, a direct output is still to be written
+    if (k0 >= k1 && !a.direct) return;
   }
   if (c1 > c0) {
     // this tile's RT of the candidates whose query head belongs to key head h (and, for the shared rows, whose
@@ -166,7 +270,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
     for (int b = c0; b < c1 && seen < (tile + 1) * RT; b += kPaNT) {
       const int c = b + tid;
       bool mine = c < c1 && min(max(a.heads[c], 0), a.g.H * a.G - 1) / a.G == h;
-      if (shared && mine) mine = min(a.pos[c / a.n], a.max_len - 1) + 1 >= a.P;
+      if (shared && mine) mine = pa_len(a, c / a.n) >= a.P;
       int total;
       const int at = seen + block_excl_scan<kPaNT>(mine ? 1 : 0, red, &total) - tile * RT;
       if (mine && at >= 0 && at < RT) rows[at] = c;
@@ -181,19 +285,34 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
     const unsigned long long on = __ballot(r >= 0);
     if (on == 0) return;
     nr = 64 - __builtin_clzll(on);
-    first = rows[__builtin_ctzll(on)];
+    first = __builtin_amdgcn_readfirstlane(rows[__builtin_ctzll(on)]);
+  }
+  // (scalars: every thread has the same)
+  k0 = __builtin_amdgcn_readfirstlane(k0);
+  k1 = __builtin_amdgcn_readfirstlane(k1);
+  h = __builtin_amdgcn_readfirstlane(h);
+  lead = __builtin_amdgcn_readfirstlane(lead);
+  group = __builtin_amdgcn_readfirstlane(group);
+  if (k0 >= k1) {                                      // (direct only) nothing attended: 0, log of 0
+    for (int x = tid; x < nr * a.ldo; x += kPaNT) {
+      const int r = x / a.ldo, d = x - r * a.ldo;
+      a.out[(int64_t)rows[r] * a.ldo + d] = a.ldo != a.g.dh && d == 1 ? 1.f : 0.f;
+      if (d == 0 && a.lse != nullptr) a.lse[rows[r]] = -INFINITY;
+    }
+    return;
   }
   const int t_first = first / a.n;
   const int sq = min(max(a.seq != nullptr ? a.seq[t_first] : t_first, 0), a.g.n_seq - 1);
   const int32_t* trow = a.g.table + (int64_t)sq * a.g.max_pages;
-  const char* Kh = a.g.K + h * a.g.hs;
-  const char* Vh = a.g.V + h * a.g.hs;
-  const int rowb = a.g.dh * EB;
+  const int rowb = FULL ? DH * EB : a.g.dh * EB;
+  // this lane's piece of a key, chunk of a value (FULL: the others are at constant distances)
+  const char* Kh = a.g.K + h * a.g.hs + (FULL ? grp * 16 : 0);
+  const char* Vh = a.g.V + h * a.g.hs + (FULL ? col * CH * EB : 0);
 
-  // ---- steps of this wavefront: cache rows key_of(i) .. + SK
+  // ---- steps of this wavefront: cache rows key_of(i) .. + SK; at least one (rows past the end are masked, their loads
+  // go to the last row: every wavefront and step runs the same path, so the waits count its own loads exactly)
   auto key_of = [&](int i) { return k0 + (i * kPaNW + wave) * SK; };
-  const int left = k1 - key_of(0);
-  const int nsteps = left > 0 ? (left + kPaNW * SK - 1) / (kPaNW * SK) : 0;
+  const int nsteps = max(1, (k1 - key_of(0) + kPaNW * SK - 1) / (kPaNW * SK));
   auto page_load = [&](int i) {
     int row;
     return trow[page_of(a.g, min(key_of(i) + (lane & (SK - 1)), k1 - 1), &row)];
@@ -214,7 +333,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
       const char* p = Kh + offs[wave][buf][u * 16 + col];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const char* pp = p + min(ks * 64 + grp * 16, rowb - 16);
+        const char* pp = p + (FULL ? ks * 64 : min(ks * 64 + grp * 16, rowb - 16));
         kr[u][ks] = QT == 0 ? ld_stream(pp) : ld_plain(pp);
       }
     }
@@ -225,48 +344,56 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
       const char* p = Vh + offs[wave][buf][(i >> 2) * 16 + grp * 4 + (i & 3)];
 #pragma unroll
       for (int m = 0; m < M; ++m) {
-        const VT* pp = reinterpret_cast<const VT*>(p + min((m * 16 + col) * (int)sizeof(VT), rowb - (int)sizeof(VT)));
+        const VT* pp = reinterpret_cast<const VT*>(
+            p + (FULL ? m * 16 * (int)sizeof(VT) : min((m * 16 + col) * (int)sizeof(VT), rowb - (int)sizeof(VT))));
         vr[i][m] = QT == 0 ? __builtin_nontemporal_load(pp) : *pp;
       }
     }
   };
-  int id1 = 0;
-  if (nsteps > 0) {
-    place(0, page_load(0), 0);
-    if (nsteps > 1) id1 = page_load(1);
-    load_k(0);
-    load_v(0);
-  }
-
-  // ---- queries: scaled halves (fp16) or as they are, and the factor >= 0 from products to base-2 logits (a negative
-  // scale's sign goes to the queries)
-  const float sign = a.scale < 0.f ? -1.f : 1.f;
-  u32x4 qh[NT][KS], ql[NT][SPLIT || !F16 ? 1 : KS];
-  float cf[NT];
+  // ---- queries, asked for before the first keys and values (loads return in order)
+  constexpr int Q4 = F16 ? 2 : 1;                      // float4 of a piece
+  f32x4 x[NT][KS][Q4];
+  int klim[NT], ktok[NT];                              // end of a column's rows, its token in the group
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = SPLIT ? col & 7 : nt * 16 + col;
     const int idx = rows[r];
     const float* qp = a.q + (int64_t)max(idx, 0) * a.g.dh;
-    constexpr int Q4 = F16 ? 2 : 1;                    // float4 of a piece
-    f32x4 x[KS][Q4];
-    float mx = 0.f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int i = 0; i < Q4; ++i) {
         const int d = ks * 16 * Q4 + grp * 4 * Q4 + i * 4;
-        const bool on = idx >= 0 && d < a.g.dh;
         const f32x4 v = *reinterpret_cast<const f32x4*>(qp + min(d, a.g.dh - 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[ks][i][e] = on ? v[e] : 0.f;
-          mx = fmaxf(mx, fabsf(x[ks][i][e]));
-        }
+        x[nt][ks][i] = idx >= 0 && d < a.g.dh ? v : f32x4{0.f, 0.f, 0.f, 0.f};
       }
+    klim[nt] = k1;
+    ktok[nt] = 0;
+    if (group > 1 && idx >= 0) {
+      ktok[nt] = idx / a.n - lead;
+      klim[nt] = min(k1, pa_len(a, lead + ktok[nt]));
+    }
+  }
+  const int kmin = group > 1 ? min(k1, pa_len(a, lead)) : k1;   // (ascending: the first has the fewest)
+  place(0, page_load(0), 0);
+  int id1 = page_load(1);
+  load_k(0);
+  load_v(0);
+  // scaled halves (fp16) or as they are, and the factor >= 0 from products to base-2 logits (a negative
+  // scale's sign goes to the queries)
+  const float sign = a.scale < 0.f ? -1.f : 1.f;
+  u32x4 qh[Sh::QALL ? 1 : NT][Sh::QALL ? 1 : KS], ql[NT][SPLIT || !F16 || Sh::QLO ? 1 : KS];
+  u32x4* qlds = reinterpret_cast<u32x4*>(smem) + lane;  // [first, second half][nt][ks][lane], the same from every wavefront
+  float cf[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
     if constexpr (F16) {
-      mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+      float mx = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[nt][ks][e >> 2][e & 3]));
+      mx = pa_max_groups(mx);
       const int ex = 14 - ((int)((__float_as_uint(mx) >> 23) & 255u) - 127);   // largest element to [2^14, 2^15)
       cf[nt] = ldexpf(fabsf(a.scale), -ex);
 #pragma unroll
@@ -274,21 +401,33 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
         f16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float v = ldexpf(sign * x[ks][e >> 2][e & 3], ex);
+          const float v = ldexpf(sign * x[nt][ks][e >> 2][e & 3], ex);
           hi[e] = (_Float16)v;
           lo[e] = (_Float16)(v - (float)hi[e]);
         }
         if constexpr (SPLIT) {
           qh[nt][ks] = col < 8 ? __builtin_bit_cast(u32x4, hi) : __builtin_bit_cast(u32x4, lo);
         } else {
-          qh[nt][ks] = __builtin_bit_cast(u32x4, hi);
-          ql[nt][ks] = __builtin_bit_cast(u32x4, lo);
+          if constexpr (Sh::QALL)
+            qlds[(nt * KS + ks) * kWave] = __builtin_bit_cast(u32x4, hi);
+          else
+            qh[nt][ks] = __builtin_bit_cast(u32x4, hi);
+          if constexpr (Sh::QLO)
+            qlds[((NT + nt) * KS + ks) * kWave] = __builtin_bit_cast(u32x4, lo);
+          else
+            ql[nt][ks] = __builtin_bit_cast(u32x4, lo);
         }
       }
     } else {
       cf[nt] = fabsf(a.scale);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) qh[nt][ks] = __builtin_bit_cast(u32x4, x[ks][0] * sign);
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 v = __builtin_bit_cast(u32x4, x[nt][ks][0] * sign);
+        if constexpr (Sh::QALL)
+          qlds[(nt * KS + ks) * kWave] = v;
+        else
+          qh[nt][ks] = v;
+      }
     }
   }
 
@@ -304,47 +443,49 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
   }
   for (int i = 0; i < nsteps; ++i) {
     const int base = key_of(i);
-    const bool tail = base + SK > k1;
+    const bool tail = base + SK > kmin;                // rows of the step are behind the end of a column's rows
     f32x4 s[NT][SK / 16];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      if (nt > 0 && nt * 16 >= nr) break;
+    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int u = 0; u < SK / 16; ++u) {
         s[nt][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 q0 = Sh::QALL ? qlds[(nt * KS + ks) * kWave] : qh[Sh::QALL ? 0 : nt][Sh::QALL ? 0 : ks];
           if constexpr (F16) {
-            s[nt][u] = pa_mfma(kr[u][ks], qh[nt][ks], s[nt][u]);
-            if constexpr (!SPLIT) s[nt][u] = pa_mfma(kr[u][ks], ql[nt][ks], s[nt][u]);
+            s[nt][u] = pa_mfma(kr[u][ks], q0, s[nt][u]);
+            if constexpr (!SPLIT)
+              s[nt][u] = pa_mfma(kr[u][ks], Sh::QLO ? qlds[((NT + nt) * KS + ks) * kWave] : ql[nt][Sh::QLO ? 0 : ks], s[nt][u]);
           } else {
-            s[nt][u] = pa_mfma4(__builtin_bit_cast(f32x4, kr[u][ks]), __builtin_bit_cast(f32x4, qh[nt][ks]), s[nt][u]);
+            s[nt][u] = pa_mfma4(__builtin_bit_cast(f32x4, kr[u][ks]), __builtin_bit_cast(f32x4, q0), s[nt][u]);
           }
         }
       }
-    }
     // the next step's keys take the registers of this one's; its values follow behind the value products
-    if (i + 1 < nsteps) {
-      place(i + 1, id1, (i + 1) & 1);
-      if (i + 2 < nsteps) id1 = page_load(i + 2);
-      load_k((i + 1) & 1);
-    }
+    place(i + 1, id1, (i + 1) & 1);
+    id1 = page_load(i + 2);
+    load_k((i + 1) & 1);
     u32x4 ph[NT], pl[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      if (nt > 0 && nt * 16 >= nr) break;
       if constexpr (SPLIT) {
 #pragma unroll
         for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[nt][u][e] += pa_xor8(s[nt][u][e]);
       }
+      if (tail) {
+#pragma unroll
+        for (int u = 0; u < SK / 16; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[nt][u][e] = base + u * 16 + grp * 4 + e < klim[nt] ? s[nt][u][e] : -INFINITY;
+      }
       float mx = -INFINITY;
 #pragma unroll
       for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!tail || base + u * 16 + grp * 4 + e < k1) mx = fmaxf(mx, s[nt][u][e]);
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[nt][u][e]);
       mx = pa_max_groups(mx) * cf[nt];
       if (__any(mx > m[nt])) {
         const float mn = fmaxf(m[nt], mx);
@@ -361,7 +502,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           float p = __builtin_amdgcn_exp2f(fmaf(s[nt][u][e], cf[nt], -mu));
-          if (tail) p = base + u * 16 + grp * 4 + e < k1 ? p : 0.f;
+          if (tail) p = base + u * 16 + grp * 4 + e < klim[nt] ? p : 0.f;
           l[nt] += p;
           s[nt][u][e] = p;
         }
@@ -387,45 +528,58 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
         ph[nt] = __builtin_bit_cast(u32x4, s[nt][0]);
       }
     }
-    if (tail) {                                        // values behind the last row may be anything
+    // Values behind a token's rows may be anything, and 0 times infinity is not 0: there token by token, from the
+    // one with the most rows, with what is behind its rows zeroed.
+    for (int g = tail ? group - 1 : 0; g >= 0; --g) {
+      if (tail) {
+        const int end = group > 1 ? min(k1, pa_len(a, lead + g)) : k1;
 #pragma unroll
-      for (int k = 0; k < NK; ++k)
-        if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= k1)
+        for (int k = 0; k < NK; ++k)
+          if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= end)
 #pragma unroll
-          for (int mm = 0; mm < M; ++mm) vr[k][mm] = VT{};
-    }
+            for (int mm = 0; mm < M; ++mm) vr[k][mm] = VT{};
+      }
+      u32x4 th[NT], tl[NT];
 #pragma unroll
-    for (int mm = 0; mm < M; ++mm)
+      for (int nt = 0; nt < NT; ++nt) {
+        const bool other = tail && ktok[nt] != g;
 #pragma unroll
-      for (int e = 0; e < CH; ++e) {
-        if constexpr (F16) {
-          // element e of the lane's chunks of its eight rows, two to a register
-          u32x4 v;
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            v[k] = __builtin_amdgcn_perm(vr[2 * k + 1][mm][e >> 1], vr[2 * k][mm][e >> 1],
-                                         e & 1 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0 && nt * 16 >= nr) break;
-            o[nt][mm * CH + e] = pa_mfma(v, ph[nt], o[nt][mm * CH + e]);
-            if constexpr (!SPLIT) o[nt][mm * CH + e] = pa_mfma(v, pl[nt], o[nt][mm * CH + e]);
-          }
-        } else {
-          f32x4 v;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(vr[k][mm][e]);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            if (nt > 0 && nt * 16 >= nr) break;
-            o[nt][mm * CH + e] = pa_mfma4(v, __builtin_bit_cast(f32x4, ph[nt]), o[nt][mm * CH + e]);
-          }
+        for (int j = 0; j < 4; ++j) {
+          th[nt][j] = other ? 0u : ph[nt][j];
+          if constexpr (F16 && !SPLIT) tl[nt][j] = other ? 0u : pl[nt][j];
         }
       }
-    if (i + 1 < nsteps) load_v((i + 1) & 1);
+#pragma unroll
+      for (int mm = 0; mm < M; ++mm)
+#pragma unroll
+        for (int e = 0; e < CH; ++e) {
+          if constexpr (F16) {
+            // element e of the lane's chunks of its eight rows, two to a register
+            u32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              v[k] = __builtin_amdgcn_perm(vr[2 * k + 1][mm][e >> 1], vr[2 * k][mm][e >> 1],
+                                           e & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              o[nt][mm * CH + e] = pa_mfma(v, th[nt], o[nt][mm * CH + e]);
+              if constexpr (!SPLIT) o[nt][mm * CH + e] = pa_mfma(v, tl[nt], o[nt][mm * CH + e]);
+            }
+          } else {
+            f32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(vr[k][mm][e]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              o[nt][mm * CH + e] = pa_mfma4(v, __builtin_bit_cast(f32x4, th[nt]), o[nt][mm * CH + e]);
+          }
+        }
+    }
+    load_v((i + 1) & 1);
   }
 
   // ---- join the wavefronts: every one writes its sums (zeros where it had no step), then all threads add
+  if constexpr (Sh::QLO || Sh::QALL) __syncthreads();  // (the queries lie there)
   float* sm_o = smem;                                  // [wave][RT][DHP]
   float* sm_m = smem + kPaNW * RT * DHP;               // [wave][RT]
   float* sm_l = sm_m + kPaNW * RT;
@@ -460,7 +614,6 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
     }
   }
   __syncthreads();
-  const bool direct = a.slots == 1 && a.P == 0;
   const int d4 = a.g.dh / 4;
   for (int x = tid; x < nr * d4; x += kPaNT) {
     const int r = x / d4, d = (x - r * d4) * 4;
@@ -482,7 +635,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
       for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], f, acc[e]);
     }
     const float me = mt - (F16 ? 14.f : 0.f);          // the sums' own factor
-    if (direct) {
+    if (a.direct) {
       const float rl = lt == 0.f ? 0.f : 1.f / lt;
       float* out = a.out + (int64_t)idx * a.ldo;
       if (a.ldo != a.g.dh) {                            // partials' form, for the out-projection
@@ -498,31 +651,63 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT>::WAVES)) k_paged_a
       if (d == 0 && a.lse != nullptr)
         a.lse[idx] = lt == 0.f ? -INFINITY : (me + __builtin_amdgcn_logf(lt)) * kPaLn2;
     } else {
-      const int64_t ps = (int64_t)idx * a.slots + slot;
-      *reinterpret_cast<f32x4*>(a.o + ps * a.g.dh + d) = acc;
+      float* po = shared ? a.so + ((int64_t)idx * a.SP + place0) * a.g.dh : a.oo + (place0 + r) * a.g.dh;
+      float* pm = shared ? a.sml + ((int64_t)idx * a.SP + place0) * 2 : a.oml + (place0 + r) * 2;
+      *reinterpret_cast<f32x4*>(po + d) = acc;
       if (d == 0) {
-        a.ml[ps * 2] = me;
-        a.ml[ps * 2 + 1] = lt;
+        pm[0] = me;
+        pm[1] = lt;
       }
     }
   }
 }
 
-// Rows' partials joined: a wavefront per row; the slots' weights in lanes, then their value sums, two slots at a
+// Rows' partials joined: a wavefront per row; the parts' weights in lanes, then their value sums, two parts at a
 // time (half a wavefront each) where a row is at most 32 chunks of four.
 __global__ void __launch_bounds__(kPaNT) k_paged_combine(PagedAttnArgs a) {
   const int idx = (int)blockIdx.x * kPaNW + (int)(threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (idx >= a.T * a.n) return;
-  const Own own = own_rows(a, idx / a.n);
-  const int b = own.start > 0 ? 0 : a.SP, e = a.SP + own.parts, ns = e - b;
-  const int64_t base = (int64_t)idx * a.slots + b;
+  const int t = idx / a.n, j = idx - t * a.n;
+  const int len = pa_len(a, t), start = pa_start(a, len);
+  // parts: [0, sp) of the shared rows, then the group's whole runs, then its rest
+  int4 meta = a.target > 0 ? a.meta[t] : int4{t, len > start ? 1 : 0, -1, t};
+  if (len == start) meta.y = 0, meta.z = -1;
+  const int sp = start > 0 ? a.SP : 0, ns = sp + meta.y + (meta.z >= 0 ? 1 : 0);
+  // the row's unit and place among the workgroup's rows
+  int u = j, r = 0;
+  if (a.heads == nullptr) {
+    const int h = j / a.G, q = (t - meta.w) * a.G + (j - h * a.G), tile = q / a.RT;
+    u = h * a.group_tiles + tile;
+    r = q - tile * a.RT;
+  } else if (a.G > 1) {
+    const int32_t* set = a.heads + (int64_t)t * a.n;
+    const int h = min(max(set[j], 0), a.g.H * a.G - 1) / a.G;
+    int rank = 0;
+    for (int b = 0; b < j; b += kWave)
+      rank += __popcll(__ballot(b + lane < j && min(max(set[min(b + lane, j)], 0), a.g.H * a.G - 1) / a.G == h));
+    u = h * a.group_tiles + rank / a.RT;
+    r = rank % a.RT;
+  }
+  auto part_ml = [&](int s) {
+    return s < sp ? a.sml + ((int64_t)idx * a.SP + s) * 2
+                  : a.oml + (((int64_t)(s - sp < meta.y ? meta.x + s - sp : meta.z) * a.U + u) * a.RW + r) * 2;
+  };
+  auto part_o = [&](int s) {
+    return s < sp ? a.so + ((int64_t)idx * a.SP + s) * a.g.dh
+                  : a.oo + (((int64_t)(s - sp < meta.y ? meta.x + s - sp : meta.z) * a.U + u) * a.RW + r) * a.g.dh;
+  };
   float w[2], m[2], l[2];
   float mt = -INFINITY;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int s = lane + 64 * i;
-    m[i] = s < ns ? a.ml[(base + s) * 2] : -INFINITY;
-    l[i] = s < ns ? a.ml[(base + s) * 2 + 1] : 0.f;
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+    if (s < ns) {
+      const float* p = part_ml(s);
+      m[i] = p[0];
+      l[i] = p[1];
+    }
     mt = fmaxf(mt, m[i]);
   }
   mt = wave_max(mt);
@@ -542,7 +727,7 @@ __global__ void __launch_bounds__(kPaNT) k_paged_combine(PagedAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int s = s0 + i * step + half, sc = min(s, ns - 1);
-      v[i] = *reinterpret_cast<const f32x4*>(a.o + (base + sc) * a.g.dh + min(d, a.g.dh - 4));
+      v[i] = *reinterpret_cast<const f32x4*>(part_o(sc) + min(d, a.g.dh - 4));
       const float f0 = __shfl(w[0], sc & 63, kWave), f1 = __shfl(w[1], sc & 63, kWave);
       f[i] = sc < 64 ? f0 : f1;
       if (s >= ns) v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -578,63 +763,75 @@ hipError_t launch_paged_combine(const PagedAttnArgs& a, hipStream_t st) {
 }
 
 // ------------------------------------------------------------------ launch
-// Query rows of a workgroup: the smallest tile that holds a unit's rows (kernel variant QT), the largest otherwise.
-static int pa_variant(int ktype, int dh, int most) {
-  const bool f16 = ktype == DV_F16;
-  if (most <= (f16 ? 8 : 16)) return 0;
-  return 2;
-}
+// Query rows of a workgroup: the smaller tile if it holds a unit's rows (kernel variant QT).
 static int pa_rows(int ktype, int qt) { return qt == 0 ? (ktype == DV_F16 ? 8 : 16) : 16 * qt; }
+static int pa_variant(int ktype, int most) { return most <= pa_rows(ktype, 0) ? 0 : 2; }
 
-static int pa_most(const PagedAttnArgs& a) {           // query rows of the largest unit
+// Query rows of the largest unit: all tokens' of a key head for the shared rows, else a token's, or those of as many
+// tokens as the table's sequences have on average.
+static int pa_most(const PagedAttnArgs& a) {
   const int own = a.heads != nullptr ? min(a.G, a.n) : a.G;
-  return a.P > 0 ? a.T * own : own;
+  if (a.P > 0) return (int)min((int64_t)a.T * own, (int64_t)INT32_MAX);
+  const int drafts = a.seq != nullptr && a.heads == nullptr ? min((a.T + a.g.n_seq - 1) / a.g.n_seq, 32) : 1;
+  return own * drafts;
 }
+
+// Workgroups that the work is shared among (per CU), least rows of one, lengths that one takes alone, tokens up to
+// which the rows are cut evenly (every workgroup looks at all positions) and units that fill the card as they are.
+constexpr int kPaPerCu = 4, kPaLeast = 256, kPaAlone = 512, kPaMaxScan = 1024;
 
 void plan_paged_attn(PagedAttnArgs* a, int ktype) {
-  const int rt = pa_rows(ktype, pa_variant(ktype, a->g.dh, pa_most(*a)));
+  const int cus = device_cu_count();
+  a->RT = pa_rows(ktype, pa_variant(ktype, pa_most(*a)));
   const int group = a->heads != nullptr ? min(a->G, a->n) : a->G;
-  a->row_tiles = a->P > 0 ? max(1, (a->T * group + rt - 1) / rt) : 0;
-  a->group_tiles = max(1, (group + rt - 1) / rt);
   const bool single = a->heads != nullptr && a->G == 1;
-  const int64_t units = (int64_t)a->T * (single ? a->n : a->g.H) * a->group_tiles;
-  const int64_t own = a->max_len - a->P;
-  // Rows of a workgroup: the whole work over about four workgroups a CU, at least 256 rows (two steps of each
-  // wavefront), so that the parts' sums stay small beside the cache rows.
+  a->row_tiles = a->P > 0 ? (int)(((int64_t)a->T * group + a->RT - 1) / a->RT) : 0;
+  a->group_tiles = (group + a->RT - 1) / a->RT;
+  a->U = single ? a->n : a->g.H * a->group_tiles;
+  const int64_t units = (int64_t)a->T * a->U, own = a->max_len - a->P;
+  const int64_t wgs = (int64_t)kPaPerCu * cus;
+  const bool whole = a->T > kPaMaxScan;
+  a->direct = a->P == 0 && (whole || own <= kPaAlone || units >= 4 * wgs);
+  a->gmax = a->seq != nullptr && a->heads == nullptr && a->group_tiles == 1 && (a->direct || !whole) ? a->RT / a->G : 1;
+  a->RW = min(a->RT, a->gmax * group);
+  // rows of a workgroup if all tokens have max_len: the shared rows' parts; a token's own are cut from its position
   const int64_t total = units * own + (int64_t)a->g.H * a->row_tiles * a->P;
-  const int64_t wgs = 4LL * device_cu_count();
-  const int64_t chunk = max((int64_t)256, (total + wgs - 1) / wgs);
-  auto parts = [&](int64_t n) { return (int)min((int64_t)kPaMaxSlots, max((int64_t)1, (n + chunk - 1) / chunk)); };
-  a->S = parts(own);
-  a->cmin = 128;
+  const int64_t chunk = max((int64_t)kPaLeast, (total + wgs - 1) / wgs);
   a->SP = 0;
   a->CP = 1;
+  int64_t shared = 0;
   if (a->P > 0) {
-    a->CP = ((a->P + parts(a->P) - 1) / parts(a->P) + 127) / 128 * 128;
+    const int64_t parts = min((int64_t)kPaMaxParts, max((int64_t)1, (a->P + chunk - 1) / chunk));
+    a->CP = (int)((a->P + parts - 1) / parts + 127) / 128 * 128;
     a->SP = (a->P + a->CP - 1) / a->CP;
+    shared = (int64_t)a->g.H * a->SP * a->row_tiles;
   }
-  a->slots = a->SP + a->S;
   a->n_shared = a->P > 0 ? (a->g.H * a->SP + 7) / 8 * 8 * a->row_tiles : 0;
+  a->cmin = kPaLeast;
+  a->target = a->direct || whole ? 0 : (int)max(wgs - shared, wgs / 4);
+  a->items = a->T + (a->target > 0 ? (a->target + a->U - 1) / a->U : 0);
+}
+
+template <typename KT, int DH, int QT, bool FULL>
+static hipError_t launch_pa(const PagedAttnArgs& a, hipStream_t st) {
+  const size_t lds = PaShape<KT, DH, QT, FULL>::lds();
+  const hipError_t e = ensure_dyn_lds(reinterpret_cast<const void*>(k_paged_attn<KT, DH, QT, FULL>), lds);
+  if (e != hipSuccess) return e;
+  launch_k((k_paged_attn<KT, DH, QT, FULL>), dim3((unsigned)(a.n_shared + (int64_t)a.items * a.U)), dim3(kPaNT), lds, st, a);
+  return hipGetLastError();
 }
 
 template <typename KT, int DH, int QT>
-static hipError_t launch_pa(const PagedAttnArgs& a, hipStream_t st) {
-  const size_t lds = PaShape<KT, DH, QT>::lds();
-  const hipError_t e = ensure_dyn_lds(reinterpret_cast<const void*>(k_paged_attn<KT, DH, QT>), lds);
-  if (e != hipSuccess) return e;
-  const bool single = a.heads != nullptr && a.G == 1;
-  const int64_t own = (int64_t)a.T * (single ? a.n : a.g.H) * a.group_tiles * a.S;
-  launch_k((k_paged_attn<KT, DH, QT>), dim3((unsigned)(a.n_shared + own)), dim3(kPaNT), lds, st, a);
-  return hipGetLastError();
+static hipError_t launch_pa_q(const PagedAttnArgs& a, hipStream_t st) {
+  return a.g.dh == DH ? launch_pa<KT, DH, QT, true>(a, st) : launch_pa<KT, DH, QT, false>(a, st);
 }
 
 template <typename KT>
 static hipError_t launch_pa_k(int ktype, const PagedAttnArgs& a, hipStream_t st) {
-  const int qt = pa_variant(ktype, a.g.dh, pa_most(a));
-  if (a.g.dh <= 64) return qt == 0 ? launch_pa<KT, 64, 0>(a, st) : qt == 2 ? launch_pa<KT, 64, 2>(a, st) : launch_pa<KT, 64, 4>(a, st);
-  if (a.g.dh <= 128)
-    return qt == 0 ? launch_pa<KT, 128, 0>(a, st) : qt == 2 ? launch_pa<KT, 128, 2>(a, st) : launch_pa<KT, 128, 4>(a, st);
-  return qt == 0 ? launch_pa<KT, 256, 0>(a, st) : launch_pa<KT, 256, 2>(a, st);
+  const bool few = a.RT == pa_rows(ktype, 0);
+  if (a.g.dh <= 64) return few ? launch_pa_q<KT, 64, 0>(a, st) : launch_pa_q<KT, 64, 2>(a, st);
+  if (a.g.dh <= 128) return few ? launch_pa_q<KT, 128, 0>(a, st) : launch_pa_q<KT, 128, 2>(a, st);
+  return few ? launch_pa_q<KT, 256, 0>(a, st) : launch_pa_q<KT, 256, 2>(a, st);
 }
 
 hipError_t launch_paged_attn(int ktype, const PagedAttnArgs& a, hipStream_t st) {
