@@ -40,92 +40,130 @@ constexpr int kPaNW = 4, kPaNT = 64 * kPaNW;
 constexpr float kPaLn2 = 0.693147180559945309f;
 constexpr int kPaMaxParts = 64;      // parts of the shared rows, and of a group's own, at most
 
-// Rows that token t attends, and how many of them are shared ones (all of those, or none: a token that attends fewer
+// Rows that a position attends, and how many of them are shared ones (all of those, or none: a token that attends fewer
 // takes what it attends by itself).
-__device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int t) { return min(max(a.pos[t], -1), a.max_len - 1) + 1; }
+__device__ __forceinline__ int pa_rows_of(const PagedAttnArgs& a, int pos) { return min(max(pos, -1), a.max_len - 1) + 1; }
+__device__ __forceinline__ int pa_len(const PagedAttnArgs& a, int t) { return pa_rows_of(a, a.pos[t]); }
 __device__ __forceinline__ int pa_start(const PagedAttnArgs& a, int len) { return a.P > 0 && len >= a.P ? a.P : 0; }
 
-// Tokens next to each other that share a sequence (drafts) are a group, whose own rows are read once: up to gmax of
-// them (aligned), at ascending positions not far apart. True for the first token of a group.
-constexpr int kPaGroupSpan = 64;
-__device__ __forceinline__ bool pa_leads(const PagedAttnArgs& a, int t) {
-  if (a.gmax == 1 || t % a.gmax == 0) return true;
-  const int p = a.pos[t], b = a.pos[t - 1];
-  return a.seq[t] != a.seq[t - 1] || b < 0 || p < b || p - b > kPaGroupSpan ||
-         pa_start(a, pa_len(a, t)) != pa_start(a, pa_len(a, t - 1));
+// Over a wavefront without LDS: row shifts and rotations, then across its rows of 16.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int pa_dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int pa_wave_incl(int v) {      // inclusive prefix sum
+  v += pa_dpp<0x111>(v);
+  v += pa_dpp<0x112>(v);
+  v += pa_dpp<0x114>(v);
+  v += pa_dpp<0x118>(v);
+  v += pa_dpp<0x142, 0xa>(v);
+  v += pa_dpp<0x143, 0xc>(v);
+  return v;
 }
-// A group's own rows, at its last token (0 at the others).
-__device__ __forceinline__ int pa_own(const PagedAttnArgs& a, int t) {
-  if (t >= a.T || (t + 1 < a.T && !pa_leads(a, t + 1))) return 0;
-  const int len = pa_len(a, t);
-  return len - pa_start(a, len);
+__device__ __forceinline__ int pa_last(int v) { return __builtin_amdgcn_readlane(v, kWave - 1); }
+__device__ __forceinline__ int pa_wave_max(int v) {       // of values >= 0, uniform
+  v = max(v, pa_dpp<0x111>(v));
+  v = max(v, pa_dpp<0x112>(v));
+  v = max(v, pa_dpp<0x114>(v));
+  v = max(v, pa_dpp<0x118>(v));
+  v = max(v, pa_dpp<0x142, 0xa>(v));
+  v = max(v, pa_dpp<0x143, 0xc>(v));
+  return pa_last(v);
+}
+
+// Tokens next to each other that share a sequence (drafts) are a group, whose own rows are read once: up to gmax of
+// them (aligned; a power of two), at ascending positions not far apart. A lane's token t:
+struct PaTok {
+  int len, seq;
+  bool leads, ends;                  // the first, the last of its group
+  int own;                           // a group's own rows, at its last token (0 at the others, and past the tokens)
+};
+constexpr int kPaGroupSpan = 64;
+__device__ __forceinline__ PaTok pa_token(const PagedAttnArgs& a, int t) {
+  const int c = min(t, a.T - 1), b = max(c - 1, 0), d = min(c + 1, a.T - 1);
+  const int pb = a.pos[b], pc = a.pos[c], pd = a.pos[d];   // (one round of loads)
+  int sb = 0, sc = c, sd = 0;
+  if (a.seq != nullptr) sc = a.seq[c];
+  if (a.gmax > 1) {
+    sb = a.seq[b];
+    sd = a.seq[d];
+  }
+  PaTok k;
+  k.len = pa_rows_of(a, pc);
+  k.seq = sc;
+  const int start = pa_start(a, k.len);
+  auto splits = [&](int s0, int p0, int s1, int p1) {
+    return s0 != s1 || p0 < 0 || p1 < p0 || p1 - p0 > kPaGroupSpan ||
+           pa_start(a, pa_rows_of(a, p0)) != pa_start(a, pa_rows_of(a, p1));
+  };
+  k.leads = (c & (a.gmax - 1)) == 0 || splits(sb, pb, sc, pc);
+  k.ends = c + 1 == a.T || ((c + 1) & (a.gmax - 1)) == 0 || splits(sc, pc, sd, pd);
+  k.own = t < a.T && k.ends ? k.len - start : 0;
+  return k;
 }
 
 // How the groups' own rows are cut: runs of `chunk` rows, chosen from what the batch attends now (every wavefront
 // computes the same), so that a.target workgroups share them evenly. Items are numbered: the whole
 // runs of all groups, then the groups' rests (the short ones last, where the last workgroups are waited for).
-struct PaCut { int chunk, whole; };
-__device__ __forceinline__ int pa_wave_incl(int v, int lane) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int n = __shfl_up(v, o, kWave);
-    if (lane >= o) v += n;
-  }
-  return v;
+// first: the lane's token of the first 64 (for more, the others are read in every pass).
+struct PaCut { int chunk, whole; float inv; };
+__device__ __forceinline__ int pa_runs(const PaCut& c, int n) {   // n / chunk (at most kPaMaxParts)
+  int q = (int)((float)n * c.inv);
+  q -= q * c.chunk > n ? 1 : 0;
+  q += n - q * c.chunk >= c.chunk ? 1 : 0;
+  return q;
 }
-__device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, int U, int lane) {
+__device__ __forceinline__ int pa_own(const PagedAttnArgs& a, const PaTok& first, int b, int lane) {
+  return b == 0 ? first.own : pa_token(a, b + lane).own;
+}
+__device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, const PaTok& first, int lane) {
   float rows = 0.f;
   int most = 0;
   for (int b = 0; b < a.T; b += kWave) {
-    const int n = pa_own(a, b + lane);
-    rows += (float)n;
-    most = max(most, n);
+    // (sums of 64 lanes in units of 64 rows: below 2^31)
+    const int n = pa_own(a, first, b, lane);
+    rows += (float)pa_last(pa_wave_incl((n + 63) >> 6)) * 64.f;
+    most = max(most, pa_wave_max(n));
   }
-  rows = wave_sum(rows);
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) most = max(most, __shfl_xor(most, o, kWave));
-  // (a little more than the even share: the rows' sum is rounded)
-  const float even = fminf(rows * 1.0001f * (float)U / (float)a.target + 1.f, 1e9f);
+  const float even = fminf(rows * (float)a.U / (float)a.target + 1.f, 1e9f);
   PaCut c;
   c.chunk = max(max(a.cmin, (int)even), most / (kPaMaxParts - 1) + 1);
   c.chunk = (c.chunk + 127) & ~127;
+  c.inv = 1.f / (float)c.chunk;
   c.whole = 0;
-  for (int b = 0; b < a.T; b += kWave) c.whole += pa_own(a, b + lane) / c.chunk;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) c.whole += __shfl_xor(c.whole, o, kWave);
+  for (int b = 0; b < a.T; b += kWave) c.whole += pa_last(pa_wave_incl(pa_runs(c, pa_own(a, first, b, lane))));
   return c;
 }
 // The group (its last token) and run of an item; -1: there is no such item.
-__device__ __forceinline__ int pa_find(const PagedAttnArgs& a, const PaCut& c, int item, int lane, int* run) {
+__device__ __forceinline__ int pa_find(const PagedAttnArgs& a, const PaTok& first, const PaCut& c, int item, int lane, int* run) {
   int seen = item < c.whole ? 0 : c.whole;
   for (int b = 0; b < a.T; b += kWave) {
-    const int n = pa_own(a, b + lane), w = n / c.chunk;
+    const int n = pa_own(a, first, b, lane), w = pa_runs(c, n);
     const int mine = item < c.whole ? w : (n - w * c.chunk > 0 ? 1 : 0);
-    const int incl = seen + pa_wave_incl(mine, lane);
+    const int incl = seen + pa_wave_incl(mine);
     const unsigned long long hit = __ballot(item < incl && item >= incl - mine);
     if (hit != 0) {
       const int l = __builtin_ctzll(hit);
-      *run = item < c.whole ? item - (__shfl(incl, l, kWave) - __shfl(mine, l, kWave)) : __shfl(w, l, kWave);
+      *run = item < c.whole ? item - __builtin_amdgcn_readlane(incl - mine, l) : __builtin_amdgcn_readlane(w, l);
       return b + l;
     }
-    seen = __shfl(incl, kWave - 1, kWave);
+    seen = pa_last(incl);
   }
   return -1;
 }
 // For the join: per token its group's first whole run, their number, the rest's item or -1, and the group's first token.
-__device__ __forceinline__ void pa_write_meta(const PagedAttnArgs& a, const PaCut& c, int lane) {
+__device__ __forceinline__ void pa_write_meta(const PagedAttnArgs& a, const PaTok& first, const PaCut& c, int lane) {
   int whole = 0, rest = c.whole;
   for (int b = 0; b < a.T; b += kWave) {
     const int t = b + lane;
-    const int n = pa_own(a, t), w = n / c.chunk, r = n - w * c.chunk > 0 ? 1 : 0;
-    const int iw = whole + pa_wave_incl(w, lane), ir = rest + pa_wave_incl(r, lane);
-    if (t < a.T && (t + 1 == a.T || pa_leads(a, t + 1))) {
-      int lead = t;
-      while (!pa_leads(a, lead)) --lead;
-      for (int m = lead; m <= t; ++m) a.meta[m] = int4{iw - w, w, r ? ir - 1 : -1, lead};
-    }
-    whole = __shfl(iw, kWave - 1, kWave);
-    rest = __shfl(ir, kWave - 1, kWave);
+    const PaTok k = b == 0 ? first : pa_token(a, t);
+    const int w = pa_runs(c, k.own), r = k.own - w * c.chunk > 0 ? 1 : 0;
+    const int iw = whole + pa_wave_incl(w), ir = rest + pa_wave_incl(r);
+    // (a group lies within 64 aligned tokens: its first is the last leading lane up to this one)
+    const unsigned long long up = __ballot(k.leads && t < a.T) & (~0ull >> (kWave - 1 - lane));
+    if (t < a.T && k.ends)
+      for (int m = b + 63 - __builtin_clzll(up); m <= t; ++m)
+        a.meta[m] = int4{iw - w, w, r ? ir - 1 : -1, b + 63 - __builtin_clzll(up)};
+    whole = pa_last(iw);
+    rest = pa_last(ir);
   }
 }
 
@@ -187,6 +225,8 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   constexpr int EB = sizeof(KT);
   __shared__ int rows[RT];
   __shared__ int red[kPaNW + 1];
+  __shared__ int glen[RT];                             // rows that the tokens of the group attend
+  __shared__ float qfac[RT];
   __shared__ int64_t offs[kPaNW][2][SK];
   extern __shared__ float smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;   // (a scalar: so are the steps)
@@ -195,6 +235,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   // ---- the unit: query rows (rows[0..nr): index t n + j, or -1), key head, cache rows [k0, k1), place of its partials
   int h, tile, k0, k1, c0 = 0, c1 = 0;                 // [c0, c1): candidates of head sets to look through
   int group = 1, lead = 0;                             // tokens of the unit (own rows), the first
+  int sq = -1;                                         // its sequence (shared rows: any that attends them)
   int64_t place0;                                      // partials: row index * SP + part, or workgroup * RW + row
   const bool shared = (int)blockIdx.x < a.n_shared;
   if (shared) {
@@ -223,20 +264,20 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
     const int item = id / a.U, u = id - item * a.U;
     int t = item, run = 0, chunk = INT32_MAX;
     if (a.target > 0) {
-      const PaCut cut = pa_cut(a, a.U, lane);
-      if (id == 0 && wave == 0) pa_write_meta(a, cut, lane);
-      t = pa_find(a, cut, item, lane, &run);
+      const PaTok tok = pa_token(a, lane);
+      const PaCut cut = pa_cut(a, tok, lane);
+      if (id == 0 && wave == 0) pa_write_meta(a, tok, cut, lane);
+      t = pa_find(a, tok, cut, item, lane, &run);
       if (t < 0) return;
       chunk = cut.chunk;
-    } else if (t + 1 < a.T && !pa_leads(a, t + 1)) {
-      return;                                          // (its group's last token takes it)
     }
-    lead = t;
-    if (a.gmax > 1) {                                  // lane k: does token t - k lead?
-      const bool first = lane < a.gmax && lane <= t && pa_leads(a, t - lane);
-      lead = t - __builtin_ctzll(__ballot(first));
-    }
+    // lane k: token t - k (its group's first is the nearest that leads; t is its group's last, or there is nothing to do)
+    const PaTok tok = pa_token(a, max(t - lane, 0));
+    if (!__builtin_amdgcn_readfirstlane((int)tok.ends)) return;
+    lead = t - (a.gmax > 1 ? __builtin_ctzll(__ballot(tok.leads)) : 0);
     group = t - lead + 1;
+    sq = __builtin_amdgcn_readfirstlane(tok.seq);
+    if (wave == 0 && lane < group) glen[group - 1 - lane] = tok.len;
     const bool single = a.heads != nullptr && a.G == 1;   // one row: the unit is (token, place in its set)
     if (single) {
       tile = 0;
@@ -255,7 +296,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
         c1 = c0 + a.n;
       }
     }
-    const int len = pa_len(a, t);
+    const int len = __builtin_amdgcn_readfirstlane(tok.len);
     k0 = pa_start(a, len) + run * (run > 0 ? chunk : 0);
     k1 = chunk < len - k0 ? k0 + chunk : len;
     place0 = (int64_t)id * a.RW;
@@ -301,8 +342,8 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
     }
     return;
   }
-  const int t_first = first / a.n;
-  const int sq = min(max(a.seq != nullptr ? a.seq[t_first] : t_first, 0), a.g.n_seq - 1);
+  if (shared) sq = a.seq != nullptr ? a.seq[first / a.n] : first / a.n;
+  sq = __builtin_amdgcn_readfirstlane(min(max(sq, 0), a.g.n_seq - 1));
   const int32_t* trow = a.g.table + (int64_t)sq * a.g.max_pages;
   const int rowb = FULL ? DH * EB : a.g.dh * EB;
   // this lane's piece of a key, chunk of a value (FULL: the others are at constant distances)
@@ -350,31 +391,36 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
       }
     }
   };
-  // ---- queries, asked for before the first keys and values (loads return in order)
+  // ---- queries, asked for before the first keys and values (loads return in order). One tile: by every wavefront for
+  // itself. More: tile w by wavefront w for all, through LDS (the space of the join)
   constexpr int Q4 = F16 ? 2 : 1;                      // float4 of a piece
-  f32x4 x[NT][KS][Q4];
-  int klim[NT], ktok[NT];                              // end of a column's rows, its token in the group
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = SPLIT ? col & 7 : nt * 16 + col;
-    const int idx = rows[r];
+  const bool mine = QT == 0 || wave < NT;
+  f32x4 x[KS][Q4];
+  if (mine) {
+    const int idx = rows[SPLIT ? col & 7 : (QT == 0 ? 0 : wave) * 16 + col];
     const float* qp = a.q + (int64_t)max(idx, 0) * a.g.dh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int i = 0; i < Q4; ++i) {
         const int d = ks * 16 * Q4 + grp * 4 * Q4 + i * 4;
-        const f32x4 v = *reinterpret_cast<const f32x4*>(qp + min(d, a.g.dh - 4));
-        x[nt][ks][i] = idx >= 0 && d < a.g.dh ? v : f32x4{0.f, 0.f, 0.f, 0.f};
+        const f32x4 v = *reinterpret_cast<const f32x4*>(qp + (FULL ? d : min(d, a.g.dh - 4)));
+        x[ks][i] = idx >= 0 && (FULL || d < a.g.dh) ? v : f32x4{0.f, 0.f, 0.f, 0.f};
       }
+  }
+  int klim[NT], ktok[NT];                              // end of a column's rows, its token in the group
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int idx = rows[SPLIT ? col & 7 : nt * 16 + col];
     klim[nt] = k1;
     ktok[nt] = 0;
     if (group > 1 && idx >= 0) {
       ktok[nt] = idx / a.n - lead;
-      klim[nt] = min(k1, pa_len(a, lead + ktok[nt]));
+      klim[nt] = min(k1, glen[ktok[nt]]);
     }
   }
-  const int kmin = group > 1 ? min(k1, pa_len(a, lead)) : k1;   // (ascending: the first has the fewest)
+  // (ascending: the first has the fewest)
+  const int kmin = __builtin_amdgcn_readfirstlane(group > 1 ? min(k1, glen[0]) : k1);
   place(0, page_load(0), 0);
   int id1 = page_load(1);
   load_k(0);
@@ -383,50 +429,59 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   // scale's sign goes to the queries)
   const float sign = a.scale < 0.f ? -1.f : 1.f;
   u32x4 qh[Sh::QALL ? 1 : NT][Sh::QALL ? 1 : KS], ql[NT][SPLIT || !F16 || Sh::QLO ? 1 : KS];
-  u32x4* qlds = reinterpret_cast<u32x4*>(smem) + lane;  // [first, second half][nt][ks][lane], the same from every wavefront
+  u32x4* qlds = reinterpret_cast<u32x4*>(smem) + lane;  // [first, second half][nt][ks][lane]
   float cf[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  if (mine) {
+    const int tq = QT == 0 ? 0 : wave;
+    float c = fabsf(a.scale);
+    int ex = 0;
     if constexpr (F16) {
       float mx = 0.f;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[nt][ks][e >> 2][e & 3]));
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, fabsf(x[ks][e >> 2][e & 3]));
       mx = pa_max_groups(mx);
-      const int ex = 14 - ((int)((__float_as_uint(mx) >> 23) & 255u) - 127);   // largest element to [2^14, 2^15)
-      cf[nt] = ldexpf(fabsf(a.scale), -ex);
+      ex = 14 - ((int)((__float_as_uint(mx) >> 23) & 255u) - 127);   // largest element to [2^14, 2^15)
+      c = ldexpf(c, -ex);
+    }
+    if constexpr (QT == 0)
+      cf[0] = c;
+    else if (grp == 0)
+      qfac[tq * 16 + col] = c;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
+    for (int ks = 0; ks < KS; ++ks) {
+      u32x4 first, second;
+      if constexpr (F16) {
         f16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float v = ldexpf(sign * x[nt][ks][e >> 2][e & 3], ex);
+          const float v = ldexpf(sign * x[ks][e >> 2][e & 3], ex);
           hi[e] = (_Float16)v;
           lo[e] = (_Float16)(v - (float)hi[e]);
         }
-        if constexpr (SPLIT) {
-          qh[nt][ks] = col < 8 ? __builtin_bit_cast(u32x4, hi) : __builtin_bit_cast(u32x4, lo);
-        } else {
-          if constexpr (Sh::QALL)
-            qlds[(nt * KS + ks) * kWave] = __builtin_bit_cast(u32x4, hi);
-          else
-            qh[nt][ks] = __builtin_bit_cast(u32x4, hi);
-          if constexpr (Sh::QLO)
-            qlds[((NT + nt) * KS + ks) * kWave] = __builtin_bit_cast(u32x4, lo);
-          else
-            ql[nt][ks] = __builtin_bit_cast(u32x4, lo);
-        }
+        first = __builtin_bit_cast(u32x4, hi);
+        second = __builtin_bit_cast(u32x4, lo);
+      } else {
+        first = second = __builtin_bit_cast(u32x4, x[ks][0] * sign);
       }
-    } else {
-      cf[nt] = fabsf(a.scale);
+      if constexpr (QT == 0) {
+        qh[0][ks] = !SPLIT || col < 8 ? first : second;
+      } else {
+        qlds[(tq * KS + ks) * kWave] = first;
+        if constexpr (F16) qlds[((NT + tq) * KS + ks) * kWave] = second;
+      }
+    }
+  }
+  if constexpr (QT > 0) {
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      cf[nt] = qfac[nt * 16 + col];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 v = __builtin_bit_cast(u32x4, x[nt][ks][0] * sign);
-        if constexpr (Sh::QALL)
-          qlds[(nt * KS + ks) * kWave] = v;
-        else
-          qh[nt][ks] = v;
+        if constexpr (!Sh::QALL) qh[nt][ks] = qlds[(nt * KS + ks) * kWave];
+        if constexpr (F16 && !Sh::QLO) ql[nt][ks] = qlds[((NT + nt) * KS + ks) * kWave];
       }
     }
   }
@@ -441,7 +496,8 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
 #pragma unroll
     for (int e = 0; e < M * CH; ++e) o[nt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  for (int i = 0; i < nsteps; ++i) {
+  auto step = [&](int i, auto last_c) {
+    constexpr bool LAST = decltype(last_c)::value;
     const int base = key_of(i);
     const bool tail = base + SK > kmin;                // rows of the step are behind the end of a column's rows
     f32x4 s[NT][SK / 16];
@@ -463,9 +519,11 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
         }
       }
     // the next step's keys take the registers of this one's; its values follow behind the value products
-    place(i + 1, id1, (i + 1) & 1);
-    id1 = page_load(i + 2);
-    load_k((i + 1) & 1);
+    if constexpr (!LAST) {
+      place(i + 1, id1, (i + 1) & 1);
+      id1 = page_load(i + 2);
+      load_k((i + 1) & 1);
+    }
     u32x4 ph[NT], pl[NT];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -532,7 +590,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
     // one with the most rows, with what is behind its rows zeroed.
     for (int g = tail ? group - 1 : 0; g >= 0; --g) {
       if (tail) {
-        const int end = group > 1 ? min(k1, pa_len(a, lead + g)) : k1;
+        const int end = group > 1 ? min(k1, glen[g]) : k1;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
           if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= end)
@@ -575,11 +633,13 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
           }
         }
     }
-    load_v((i + 1) & 1);
-  }
+    if constexpr (!LAST) load_v((i + 1) & 1);
+  };
+  for (int i = 0; i + 1 < nsteps; ++i) step(i, std::false_type{});
+  step(nsteps - 1, std::true_type{});
 
   // ---- join the wavefronts: every one writes its sums (zeros where it had no step), then all threads add
-  if constexpr (Sh::QLO || Sh::QALL) __syncthreads();  // (the queries lie there)
+  if constexpr (QT > 0) __syncthreads();               // (the queries lie there)
   float* sm_o = smem;                                  // [wave][RT][DHP]
   float* sm_m = smem + kPaNW * RT * DHP;               // [wave][RT]
   float* sm_l = sm_m + kPaNW * RT;
@@ -614,25 +674,30 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
     }
   }
   __syncthreads();
-  const int d4 = a.g.dh / 4;
-  for (int x = tid; x < nr * d4; x += kPaNT) {
-    const int r = x / d4, d = (x - r * d4) * 4;
-    const int idx = rows[r];
-    if (idx < 0) continue;
-    float mw[kPaNW], mt = -INFINITY, lt = 0.f;
+  // LPR threads a row, the rows of a pass next to each other
+  constexpr int LPR = DH / 4, RP = kPaNT / LPR;
+  const int d = tid % LPR * 4;
+#pragma unroll
+  for (int r0 = 0; r0 < RT; r0 += RP) {
+    const int r = r0 + tid / LPR;
+    const int idx = r < nr ? rows[r] : -1;             // (RT may be below RP)
+    if (idx < 0 || (!FULL && d >= a.g.dh)) continue;
+    float mw[kPaNW], lw[kPaNW], mt = -INFINITY, lt = 0.f;
+    f32x4 v[kPaNW];
 #pragma unroll
     for (int w = 0; w < kPaNW; ++w) {
       mw[w] = sm_m[w * RT + r];
+      lw[w] = sm_l[w * RT + r];
+      v[w] = *reinterpret_cast<const f32x4*>(sm_o + (w * RT + r) * DHP + d);
       mt = fmaxf(mt, mw[w]);
     }
     f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < kPaNW; ++w) {
       const float f = mw[w] == -INFINITY ? (mt == -INFINITY ? 1.f : 0.f) : __builtin_amdgcn_exp2f(mw[w] - mt);
-      lt = fmaf(sm_l[w * RT + r], f, lt);
-      const f32x4 v = *reinterpret_cast<const f32x4*>(sm_o + (w * RT + r) * DHP + d);
+      lt = fmaf(lw[w], f, lt);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], f, acc[e]);
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[w][e], f, acc[e]);
     }
     const float me = mt - (F16 ? 14.f : 0.f);          // the sums' own factor
     if (a.direct) {
@@ -644,6 +709,7 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
           out[1] = 1.f;
         }
         out += 2;
+#pragma unroll
         for (int e = 0; e < 4; ++e) out[d + e] = acc[e] * rl;
       } else {
         *reinterpret_cast<f32x4*>(out + d) = acc * rl;
@@ -792,7 +858,9 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   const int64_t wgs = (int64_t)kPaPerCu * cus;
   const bool whole = a->T > kPaMaxScan;
   a->direct = a->P == 0 && (whole || own <= kPaAlone || units >= 4 * wgs);
-  a->gmax = a->seq != nullptr && a->heads == nullptr && a->group_tiles == 1 && (a->direct || !whole) ? a->RT / a->G : 1;
+  a->gmax = 1;
+  if (a->seq != nullptr && a->heads == nullptr && (a->direct || !whole))
+    while (2 * a->gmax * a->G <= a->RT) a->gmax *= 2;
   a->RW = min(a->RT, a->gmax * group);
   // rows of a workgroup if all tokens have max_len: the shared rows' parts; a token's own are cut from its position
   const int64_t total = units * own + (int64_t)a->g.H * a->row_tiles * a->P;
