@@ -125,16 +125,40 @@ __device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, const PaTok& fir
   }
   const float even = fminf(rows * (float)a.U / (float)a.target + 1.f, 1e9f);
   PaCut c;
-  c.chunk = max(max(a.cmin, (int)even), most / (kPaMaxParts - 1) + 1);
-  c.chunk = (c.chunk + 127) & ~127;
-  c.inv = 1.f / (float)c.chunk;
-  c.whole = 0;
-  for (int b = 0; b < a.T; b += kWave) c.whole += pa_last(pa_wave_incl(pa_runs(c, pa_own(a, first, b, lane))));
+  int chunk = max(max(a.cmin, (int)even), most / (kPaMaxParts - 1) + 1);
+  // An even share gives every group a rest beside it: where the card could hold all groups at once, a quarter more rows
+  // at a time until it holds all runs and rests, which then need no second round.
+  for (int k = 0; k < 8; ++k) {
+    c.chunk = (chunk + 127) & ~127;
+    c.inv = 1.f / (float)c.chunk;
+    c.whole = 0;
+    int rests = 0, groups = 0;
+    for (int b = 0; b < a.T; b += kWave) {
+      const int n = pa_own(a, first, b, lane), w = pa_runs(c, n);
+      c.whole += pa_last(pa_wave_incl(w));
+      rests += __popcll(__ballot(n - w * c.chunk > 0));
+      groups += __popcll(__ballot(n > 0));
+    }
+    if ((int64_t)(c.whole + rests) * a.U <= a.target || (int64_t)groups * a.U > a.target) break;
+    chunk = c.chunk + (c.chunk >> 2);
+  }
   return c;
 }
 // The group (its last token) and run of an item; -1: there is no such item.
 __device__ __forceinline__ int pa_find(const PagedAttnArgs& a, const PaTok& first, const PaCut& c, int item, int lane, int* run) {
   int seen = item < c.whole ? 0 : c.whole;
+  if (item >= c.whole && a.T <= kWave) {               // rests of up to 64 tokens: the longest first
+    const int w = pa_runs(c, first.own), n = lane < a.T ? first.own - w * c.chunk : 0;
+    int rank = 0;
+    for (int l = 0; l < a.T; ++l) {
+      const int o = __builtin_amdgcn_readlane(n, l);
+      rank += o > n || (o == n && l < lane) ? 1 : 0;
+    }
+    const unsigned long long hit = __ballot(n > 0 && rank == item - c.whole);
+    if (hit == 0) return -1;
+    *run = __builtin_amdgcn_readlane(w, __builtin_ctzll(hit));
+    return __builtin_ctzll(hit);
+  }
   for (int b = 0; b < a.T; b += kWave) {
     const int n = pa_own(a, first, b, lane), w = pa_runs(c, n);
     const int mine = item < c.whole ? w : (n - w * c.chunk > 0 ? 1 : 0);
@@ -156,7 +180,16 @@ __device__ __forceinline__ void pa_write_meta(const PagedAttnArgs& a, const PaTo
     const int t = b + lane;
     const PaTok k = b == 0 ? first : pa_token(a, t);
     const int w = pa_runs(c, k.own), r = k.own - w * c.chunk > 0 ? 1 : 0;
-    const int iw = whole + pa_wave_incl(w), ir = rest + pa_wave_incl(r);
+    const int iw = whole + pa_wave_incl(w);
+    int ir = rest + pa_wave_incl(r);
+    if (a.T <= kWave) {
+      const int n = t < a.T ? k.own - w * c.chunk : 0;
+      ir = c.whole + 1;
+      for (int l = 0; l < a.T; ++l) {
+        const int o = __builtin_amdgcn_readlane(n, l);
+        ir += o > n || (o == n && l < lane) ? 1 : 0;
+      }
+    }
     // (a group lies within 64 aligned tokens: its first is the last leading lane up to this one)
     const unsigned long long up = __ballot(k.leads && t < a.T) & (~0ull >> (kWave - 1 - lane));
     if (t < a.T && k.ends)
@@ -842,41 +875,46 @@ static int pa_most(const PagedAttnArgs& a) {
   return own * drafts;
 }
 
-// Workgroups that the work is shared among (per CU), least rows of one, lengths that one takes alone, tokens up to
-// which the rows are cut evenly (every workgroup looks at all positions) and units that fill the card as they are.
-constexpr int kPaPerCu = 4, kPaLeast = 256, kPaAlone = 512, kPaMaxScan = 1024;
+// Least rows of a workgroup, lengths that one takes alone, tokens up to which the rows are cut evenly (every
+// wavefront looks at all positions).
+constexpr int kPaLeast = 256, kPaAlone = 512, kPaMaxScan = 1024;
 
 void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   const int cus = device_cu_count();
-  a->RT = pa_rows(ktype, pa_variant(ktype, pa_most(*a)));
+  const int qt = pa_variant(ktype, pa_most(*a));
+  a->RT = pa_rows(ktype, qt);
+  // workgroups that a CU holds (PaShape::WAVES)
+  const int per_cu = a->g.dh <= 64 ? (qt == 0 ? 4 : 2) : a->g.dh <= 128 ? (qt == 0 ? 3 : 2) : 1;
+  const int64_t resident = (int64_t)per_cu * cus;
   const int group = a->heads != nullptr ? min(a->G, a->n) : a->G;
   const bool single = a->heads != nullptr && a->G == 1;
   a->row_tiles = a->P > 0 ? (int)(((int64_t)a->T * group + a->RT - 1) / a->RT) : 0;
   a->group_tiles = (group + a->RT - 1) / a->RT;
   a->U = single ? a->n : a->g.H * a->group_tiles;
   const int64_t units = (int64_t)a->T * a->U, own = a->max_len - a->P;
-  const int64_t wgs = (int64_t)kPaPerCu * cus;
   const bool whole = a->T > kPaMaxScan;
-  a->direct = a->P == 0 && (whole || own <= kPaAlone || units >= 4 * wgs);
+  a->direct = a->P == 0 && (whole || own <= kPaAlone);
   a->gmax = 1;
   if (a->seq != nullptr && a->heads == nullptr && (a->direct || !whole))
     while (2 * a->gmax * a->G <= a->RT) a->gmax *= 2;
   a->RW = min(a->RT, a->gmax * group);
-  // rows of a workgroup if all tokens have max_len: the shared rows' parts; a token's own are cut from its position
-  const int64_t total = units * own + (int64_t)a->g.H * a->row_tiles * a->P;
-  const int64_t chunk = max((int64_t)kPaLeast, (total + wgs - 1) / wgs);
+  // The shared rows' parts: their share of the resident workgroups if all tokens had max_len (but no more than as many rows
+  // of their own), one a CU at least, kPaLeast rows each at least.
   a->SP = 0;
   a->CP = 1;
   int64_t shared = 0;
   if (a->P > 0) {
-    const int64_t parts = min((int64_t)kPaMaxParts, max((int64_t)1, (a->P + chunk - 1) / chunk));
+    const int64_t tiles = (int64_t)a->g.H * a->row_tiles;
+    const int64_t cost = tiles * a->P, others = units * min(own, (int64_t)a->P);
+    const int64_t want = max((int64_t)cus, resident * cost / (cost + others));
+    const int64_t parts = max((int64_t)1, min(min((int64_t)kPaMaxParts, (want + tiles - 1) / tiles), (int64_t)a->P / kPaLeast));
     a->CP = (int)((a->P + parts - 1) / parts + 127) / 128 * 128;
     a->SP = (a->P + a->CP - 1) / a->CP;
-    shared = (int64_t)a->g.H * a->SP * a->row_tiles;
+    shared = tiles * a->SP;
   }
   a->n_shared = a->P > 0 ? (a->g.H * a->SP + 7) / 8 * 8 * a->row_tiles : 0;
   a->cmin = kPaLeast;
-  a->target = a->direct || whole ? 0 : (int)max(wgs - shared, wgs / 4);
+  a->target = a->direct || whole ? 0 : (int)max(resident - shared, (int64_t)cus);
   a->items = a->T + (a->target > 0 ? (a->target + a->U - 1) / a->U : 0);
 }
 
