@@ -50,7 +50,8 @@ struct PagedAttnArgs {
   int T, n, G;                      // tokens, query heads a token, query heads a key head
   int max_len;
   float scale;                      // times log2(e)
-  int RT, U, row_tiles, group_tiles;   // query rows of a workgroup; units; tiles of a key head's shared and own rows
+  int RT, RTS;                      // query rows of a workgroup: of own rows, of the shared rows
+  int U, row_tiles, group_tiles;    // units; tiles of a key head's shared and own work
   int P, SP, CP;                    // shared rows, parts of them, rows of a part
   int n_shared;                     // workgroups of the shared rows
   int target;                       // workgroups that the own rows are cut for (0: an item is a token)

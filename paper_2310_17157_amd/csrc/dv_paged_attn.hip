@@ -249,8 +249,9 @@ __device__ __forceinline__ f32x4 pa_mfma4(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
+// One unit: of the shared rows, or of own rows.
 template <typename KT, int DH, int QT, bool FULL>
-__global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_paged_attn(PagedAttnArgs a) {
+__device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, const bool shared) {
   using Sh = PaShape<KT, DH, QT, FULL>;
   constexpr bool F16 = Sh::F16, SPLIT = Sh::SPLIT;
   constexpr int NT = Sh::NT, RT = Sh::RT, SK = Sh::SK, KS = Sh::KS, CH = Sh::CH, M = Sh::M, DHP = Sh::DHP;
@@ -261,7 +262,6 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   __shared__ int glen[RT];                             // rows that the tokens of the group attend
   __shared__ float qfac[RT];
   __shared__ int64_t offs[kPaNW][2][SK];
-  extern __shared__ float smem[];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;   // (a scalar: so are the steps)
   const int col = lane & 15, grp = lane >> 4;
 
@@ -270,7 +270,6 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   int group = 1, lead = 0;                             // tokens of the unit (own rows), the first
   int sq = -1;                                         // its sequence (shared rows: any that attends them)
   int64_t place0;                                      // partials: row index * SP + part, or workgroup * RW + row
-  const bool shared = (int)blockIdx.x < a.n_shared;
   if (shared) {
     // the row tiles of a part 8 workgroups apart: on one XCD, whose L2 then holds the part's keys and values
     const int b = blockIdx.x, x = b & 7, y = b >> 3;
@@ -761,6 +760,21 @@ __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QT, FULL>::WAVES)) k_p
   }
 }
 
+// QS, QO: variants of the shared and the own rows' units (a batch has many query rows for the shared ones, a token few).
+template <typename KT, int DH, int QS, int QO, bool FULL>
+__global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QS, FULL>::WAVES)) k_paged_attn(PagedAttnArgs a) {
+  extern __shared__ float smem[];
+  const bool shared = (int)blockIdx.x < a.n_shared;
+  if constexpr (QS == QO) {
+    pa_unit<KT, DH, QS, FULL>(a, smem, shared);
+  } else {
+    if (shared)
+      pa_unit<KT, DH, QS, FULL>(a, smem, true);
+    else
+      pa_unit<KT, DH, QO, FULL>(a, smem, false);
+  }
+}
+
 // Rows' partials joined: a wavefront per row; the parts' weights in lanes, then their value sums, two parts at a
 // time (half a wavefront each) where a row is at most 32 chunks of four.
 __global__ void __launch_bounds__(kPaNT) k_paged_combine(PagedAttnArgs a) {
@@ -864,13 +878,12 @@ hipError_t launch_paged_combine(const PagedAttnArgs& a, hipStream_t st) {
 // ------------------------------------------------------------------ launch
 // Query rows of a workgroup: the smaller tile if it holds a unit's rows (kernel variant QT).
 static int pa_rows(int ktype, int qt) { return qt == 0 ? (ktype == DV_F16 ? 8 : 16) : 16 * qt; }
-static int pa_variant(int ktype, int most) { return most <= pa_rows(ktype, 0) ? 0 : 2; }
+static int pa_variant(int ktype, int64_t most) { return most <= pa_rows(ktype, 0) ? 0 : 2; }
 
-// Query rows of the largest unit: all tokens' of a key head for the shared rows, else a token's, or those of as many
-// tokens as the table's sequences have on average.
-static int pa_most(const PagedAttnArgs& a) {
+// Query rows of the largest unit of own rows: a token's of a key head, or those of as many tokens as the table's sequences
+// have on average.
+static int pa_own_rows(const PagedAttnArgs& a) {
   const int own = a.heads != nullptr ? min(a.G, a.n) : a.G;
-  if (a.P > 0) return (int)min((int64_t)a.T * own, (int64_t)INT32_MAX);
   const int drafts = a.seq != nullptr && a.heads == nullptr ? min((a.T + a.g.n_seq - 1) / a.g.n_seq, 32) : 1;
   return own * drafts;
 }
@@ -881,14 +894,17 @@ constexpr int kPaLeast = 256, kPaAlone = 512, kPaMaxScan = 1024;
 
 void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   const int cus = device_cu_count();
-  const int qt = pa_variant(ktype, pa_most(*a));
-  a->RT = pa_rows(ktype, qt);
+  const int group = a->heads != nullptr ? min(a->G, a->n) : a->G;
+  const int qs = a->P > 0 ? pa_variant(ktype, (int64_t)a->T * group) : 0;
+  // (one token attends the shared rows with as many query rows as its own)
+  const int qo = min(pa_variant(ktype, pa_own_rows(*a)), a->P > 0 ? qs : 2), qt = max(qs, qo);
+  a->RT = pa_rows(ktype, qo);
+  a->RTS = pa_rows(ktype, qs);
   // workgroups that a CU holds (PaShape::WAVES)
   const int per_cu = a->g.dh <= 64 ? (qt == 0 ? 4 : 2) : a->g.dh <= 128 ? (qt == 0 ? 3 : 2) : 1;
   const int64_t resident = (int64_t)per_cu * cus;
-  const int group = a->heads != nullptr ? min(a->G, a->n) : a->G;
   const bool single = a->heads != nullptr && a->G == 1;
-  a->row_tiles = a->P > 0 ? (int)(((int64_t)a->T * group + a->RT - 1) / a->RT) : 0;
+  a->row_tiles = a->P > 0 ? (int)(((int64_t)a->T * group + a->RTS - 1) / a->RTS) : 0;
   a->group_tiles = (group + a->RT - 1) / a->RT;
   a->U = single ? a->n : a->g.H * a->group_tiles;
   const int64_t units = (int64_t)a->T * a->U, own = a->max_len - a->P;
@@ -918,26 +934,30 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   a->items = a->T + (a->target > 0 ? (a->target + a->U - 1) / a->U : 0);
 }
 
-template <typename KT, int DH, int QT, bool FULL>
+template <typename KT, int DH, int QS, int QO, bool FULL>
 static hipError_t launch_pa(const PagedAttnArgs& a, hipStream_t st) {
-  const size_t lds = PaShape<KT, DH, QT, FULL>::lds();
-  const hipError_t e = ensure_dyn_lds(reinterpret_cast<const void*>(k_paged_attn<KT, DH, QT, FULL>), lds);
+  const size_t lds = PaShape<KT, DH, QS, FULL>::lds();
+  const hipError_t e = ensure_dyn_lds(reinterpret_cast<const void*>(k_paged_attn<KT, DH, QS, QO, FULL>), lds);
   if (e != hipSuccess) return e;
-  launch_k((k_paged_attn<KT, DH, QT, FULL>), dim3((unsigned)(a.n_shared + (int64_t)a.items * a.U)), dim3(kPaNT), lds, st, a);
+  launch_k((k_paged_attn<KT, DH, QS, QO, FULL>), dim3((unsigned)(a.n_shared + (int64_t)a.items * a.U)), dim3(kPaNT), lds, st, a);
   return hipGetLastError();
 }
 
-template <typename KT, int DH, int QT>
+template <typename KT, int DH, int QS, int QO>
 static hipError_t launch_pa_q(const PagedAttnArgs& a, hipStream_t st) {
-  return a.g.dh == DH ? launch_pa<KT, DH, QT, true>(a, st) : launch_pa<KT, DH, QT, false>(a, st);
+  return a.g.dh == DH ? launch_pa<KT, DH, QS, QO, true>(a, st) : launch_pa<KT, DH, QS, QO, false>(a, st);
+}
+
+template <typename KT, int QS, int QO>
+static hipError_t launch_pa_d(const PagedAttnArgs& a, hipStream_t st) {
+  if (a.g.dh <= 64) return launch_pa_q<KT, 64, QS, QO>(a, st);
+  return a.g.dh <= 128 ? launch_pa_q<KT, 128, QS, QO>(a, st) : launch_pa_q<KT, 256, QS, QO>(a, st);
 }
 
 template <typename KT>
 static hipError_t launch_pa_k(int ktype, const PagedAttnArgs& a, hipStream_t st) {
-  const bool few = a.RT == pa_rows(ktype, 0);
-  if (a.g.dh <= 64) return few ? launch_pa_q<KT, 64, 0>(a, st) : launch_pa_q<KT, 64, 2>(a, st);
-  if (a.g.dh <= 128) return few ? launch_pa_q<KT, 128, 0>(a, st) : launch_pa_q<KT, 128, 2>(a, st);
-  return few ? launch_pa_q<KT, 256, 0>(a, st) : launch_pa_q<KT, 256, 2>(a, st);
+  if (a.RT > pa_rows(ktype, 0)) return launch_pa_d<KT, 2, 2>(a, st);
+  return a.P > 0 && a.RTS > pa_rows(ktype, 0) ? launch_pa_d<KT, 2, 0>(a, st) : launch_pa_d<KT, 0, 0>(a, st);
 }
 
 hipError_t launch_paged_attn(int ktype, const PagedAttnArgs& a, hipStream_t st) {
