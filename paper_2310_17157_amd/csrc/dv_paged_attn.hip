@@ -201,7 +201,7 @@ __device__ __forceinline__ void pa_write_meta(const PagedAttnArgs& a, const PaTo
 }
 
 // FULL: heads are DH elements wide (else up to DH, pieces past a row's end read its last bytes again).
-template <typename KT, int DH, int QT, bool FULL>
+template <typename KT, int DH, int QT, bool FULL, int SHARED = -1>
 struct PaShape {
   static constexpr bool F16 = std::is_same<KT, _Float16>::value;
   static constexpr bool SPLIT = F16 && QT == 0;       // both halves of a query in one tile
@@ -216,7 +216,9 @@ struct PaShape {
   // loads before it, the next step's among them)
   static constexpr int WAVES = DH == 64 ? (QT == 0 ? 4 : 2) : DH == 128 ? (QT == 0 && FULL ? 3 : 2) : 1;
   // queries in LDS (the space of the join) instead of registers: their second halves, or all
-  static constexpr bool QLO = F16 && QT == 2 && DH >= 128, QALL = QT == 2 && DH == 256;
+  // (own rows, whose steps also tell the tokens of a group apart: all)
+  static constexpr bool QLO = F16 && QT == 2 && DH >= 128;
+  static constexpr bool QALL = QT == 2 && (DH == 256 || (F16 && DH == 128 && SHARED == 0));
   static constexpr size_t lds() { return (size_t)kPaNW * RT * (DHP + 2) * sizeof(float); }
 };
 
@@ -250,9 +252,10 @@ __device__ __forceinline__ f32x4 pa_mfma4(f32x4 a, f32x4 b, f32x4 c) {
 }
 
 // One unit: of the shared rows, or of own rows.
-template <typename KT, int DH, int QT, bool FULL>
-__device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, const bool shared) {
-  using Sh = PaShape<KT, DH, QT, FULL>;
+// SHARED: 1 or 0 where the kernel knows, -1 where the workgroup does.
+template <typename KT, int DH, int QT, bool FULL, int SHARED>
+__device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem) {
+  using Sh = PaShape<KT, DH, QT, FULL, SHARED>;
   constexpr bool F16 = Sh::F16, SPLIT = Sh::SPLIT;
   constexpr int NT = Sh::NT, RT = Sh::RT, SK = Sh::SK, KS = Sh::KS, CH = Sh::CH, M = Sh::M, DHP = Sh::DHP;
   constexpr int NK = F16 ? 8 : 4;                      // cache rows of a lane in the value product
@@ -270,6 +273,7 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
   int group = 1, lead = 0;                             // tokens of the unit (own rows), the first
   int sq = -1;                                         // its sequence (shared rows: any that attends them)
   int64_t place0;                                      // partials: row index * SP + part, or workgroup * RW + row
+  const bool shared = SHARED < 0 ? (int)blockIdx.x < a.n_shared : SHARED == 1;
   if (shared) {
     // the row tiles of a part 8 workgroups apart: on one XCD, whose L2 then holds the part's keys and values
     const int b = blockIdx.x, x = b & 7, y = b >> 3;
@@ -531,7 +535,8 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
   auto step = [&](int i, auto last_c) {
     constexpr bool LAST = decltype(last_c)::value;
     const int base = key_of(i);
-    const bool tail = base + SK > kmin;                // rows of the step are behind the end of a column's rows
+    // rows of the step are behind the end of a column's rows (of a group of one: in the last step alone)
+    const bool tail = (SHARED != 1 || LAST) && base + SK > kmin;
     f32x4 s[NT][SK / 16];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -565,18 +570,19 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
 #pragma unroll
           for (int e = 0; e < 4; ++e) s[nt][u][e] += pa_xor8(s[nt][u][e]);
       }
-      if (tail) {
-#pragma unroll
-        for (int u = 0; u < SK / 16; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[nt][u][e] = base + u * 16 + grp * 4 + e < klim[nt] ? s[nt][u][e] : -INFINITY;
-      }
+      // (scaled before the maximum is taken: a product needs no quieting of NaN, which would be an instruction each)
       float mx = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < SK / 16; ++u)
+      for (int u = 0; u < SK / 16; ++u) {
+        s[nt][u] *= cf[nt];
+        if (tail) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[nt][u][e]);
-      mx = pa_max_groups(mx) * cf[nt];
+          for (int e = 0; e < 4; ++e) s[nt][u][e] = base + u * 16 + grp * 4 + e < klim[nt] ? s[nt][u][e] : -INFINITY;
+        }
+        mx = fmaxf(fmaxf(mx, s[nt][u][0]), s[nt][u][1]);
+        mx = fmaxf(fmaxf(mx, s[nt][u][2]), s[nt][u][3]);
+      }
+      mx = pa_max_groups(mx);
       if (__any(mx > m[nt])) {
         const float mn = fmaxf(m[nt], mx);
         const float f = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[nt] - mn);
@@ -591,8 +597,7 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
       for (int u = 0; u < SK / 16; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float p = __builtin_amdgcn_exp2f(fmaf(s[nt][u][e], cf[nt], -mu));
-          if (tail) p = base + u * 16 + grp * 4 + e < klim[nt] ? p : 0.f;
+          const float p = __builtin_amdgcn_exp2f(s[nt][u][e] - mu);
           l[nt] += p;
           s[nt][u][e] = p;
         }
@@ -603,7 +608,7 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
         for (int j = 0; j < 4; ++j) {
           const float p0 = s[nt][j >> 1][(j & 1) * 2], p1 = s[nt][j >> 1][(j & 1) * 2 + 1];
           const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(p0, p1));
-          const f16x2 r = {(_Float16)fmaf((float)h[0], -1.f, p0), (_Float16)fmaf((float)h[1], -1.f, p1)};
+          const f16x2 r = {(_Float16)(p0 - (float)h[0]), (_Float16)(p1 - (float)h[1])};
           hi[j] = __builtin_bit_cast(uint32_t, h);
           lo[j] = __builtin_bit_cast(uint32_t, r);
         }
@@ -764,14 +769,13 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem, con
 template <typename KT, int DH, int QS, int QO, bool FULL>
 __global__ void __launch_bounds__(kPaNT, (PaShape<KT, DH, QS, FULL>::WAVES)) k_paged_attn(PagedAttnArgs a) {
   extern __shared__ float smem[];
-  const bool shared = (int)blockIdx.x < a.n_shared;
-  if constexpr (QS == QO) {
-    pa_unit<KT, DH, QS, FULL>(a, smem, shared);
+  if constexpr (QS == 0) {
+    pa_unit<KT, DH, 0, FULL, -1>(a, smem);
   } else {
-    if (shared)
-      pa_unit<KT, DH, QS, FULL>(a, smem, true);
+    if ((int)blockIdx.x < a.n_shared)
+      pa_unit<KT, DH, QS, FULL, 1>(a, smem);
     else
-      pa_unit<KT, DH, QO, FULL>(a, smem, false);
+      pa_unit<KT, DH, QO, FULL, 0>(a, smem);
   }
 }
 
