@@ -26,6 +26,11 @@ __device__ __forceinline__ int page_of(const Pages& g, int t, int* row) {
   return p;
 }
 
+// What divides by a number that the host knows: a product and a shift.
+struct Divisor {
+  uint32_t m; int s;
+};
+
 // Rotation and append of T tokens: rotated (or copied) queries, keys and values into pages.
 struct RopeArgs {
   int T, dh, rot; const double* freq; float mscale; bool inverse;
@@ -35,8 +40,9 @@ struct RopeArgs {
   const void* k; const void* v; int64_t ldk, ldv;
   const int32_t* seq; const int32_t* heads; int nk;                  // key/value heads written a token
   Pages g;
-  // set by the launcher: tokens of a workgroup, parts of a token's work, units of a q or k head and of a v head
-  int tpw, parts, uq, uv;
+  // set by the launcher: tokens of a workgroup, parts of their work, units of a token, of a q or k head and of a v head
+  int tpw, parts, per, uq, uv;
+  Divisor by_parts, by_per, by_uq, by_uv;
 };
 hipError_t launch_rope(int xtype, int ktype, int layout, const RopeArgs& a, hipStream_t st);
 
