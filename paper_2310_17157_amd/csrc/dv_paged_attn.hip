@@ -624,10 +624,37 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem) {
       }
     }
     // Values behind a token's rows may be anything, and 0 times infinity is not 0: there token by token, from the
-    // one with the most rows, with what is behind its rows zeroed.
+    // one with the most rows, with what is behind its rows zeroed and the other tokens' probabilities 0. What is not finite
+    // would still reach their sums: such pieces are zeroed first, and the tokens that attend one of those rows get
+    // probabilities of NaN.
+    int first_bad = INT_MAX;
+    if (tail && group > 1) {
+#pragma unroll
+      for (int k = 0; k < NK; ++k) {
+        const int row = base + (k >> 2) * 16 + grp * 4 + (k & 3);
+        uint32_t bad = 0;
+#pragma unroll
+        for (int mm = 0; mm < M; ++mm)
+#pragma unroll
+          for (int w = 0; w < (int)(sizeof(VT) / 4); ++w)
+            if constexpr (F16)
+              bad |= (vr[k][mm][w] & 0x7c007c00u) + 0x04000400u;   // bit 15 or 31: an exponent of all ones
+            else
+              bad |= (vr[k][mm][w] & 0x7f800000u) + 0x00800000u;   // bit 31
+        if (bad & (F16 ? 0x80008000u : 0x80000000u)) {
+          if (row < k1) first_bad = min(first_bad, row);
+#pragma unroll
+          for (int mm = 0; mm < M; ++mm) vr[k][mm] = VT{};
+        }
+      }
+      for (int i = 1; i < kWave; i *= 2) first_bad = min(first_bad, __shfl_xor(first_bad, i, kWave));
+      first_bad = __builtin_amdgcn_readfirstlane(first_bad);
+    }
     for (int g = tail ? group - 1 : 0; g >= 0; --g) {
+      uint32_t nan = 0;
       if (tail) {
         const int end = group > 1 ? min(k1, glen[g]) : k1;
+        if (first_bad < end) nan = F16 ? 0x7e007e00u : 0x7fc00000u;
 #pragma unroll
         for (int k = 0; k < NK; ++k)
           if (base + (k >> 2) * 16 + grp * 4 + (k & 3) >= end)
@@ -637,11 +664,11 @@ __device__ __forceinline__ void pa_unit(const PagedAttnArgs& a, float* smem) {
       u32x4 th[NT], tl[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const bool other = tail && ktok[nt] != g;
+        const uint32_t own = tail && ktok[nt] != g ? 0u : ~0u;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          th[nt][j] = other ? 0u : ph[nt][j];
-          if constexpr (F16 && !SPLIT) tl[nt][j] = other ? 0u : pl[nt][j];
+          th[nt][j] = (ph[nt][j] & own) | (nan & own);
+          if constexpr (F16 && !SPLIT) tl[nt][j] = (pl[nt][j] & own) | (nan & own);
         }
       }
 #pragma unroll

@@ -377,6 +377,62 @@ def test_attention_non_finite_stays_with_its_head():
         assert (np.abs(h64(out) - o)[good] <= 1e-4 * absv[good]).all()
 
 
+@pytest.mark.parametrize("T,shared,G,ktype", [(65, 0, 1, "f16"), (130, 5, 1, "f16"), (130, 0, 5, "f32"), (1024, 0, 1, "f16"),
+                                              (1025, 0, 1, "f16"), (1025, 3, 2, "f16"), (1300, 0, 12, "f32")])
+def test_attention_of_many_tokens(T, shared, G, ktype):
+    """More tokens than a wavefront's lanes and than the cutting looks at one by one; some long, some idle, some
+    with drafts beside them."""
+    rng = np.random.default_rng(T + G)
+    lens = [int(n) for n in rng.integers(0, 12, T)]
+    lens[3], lens[T // 2], lens[T - 1] = 700, 90, 300
+    c = make(rng, lens, 1, G, 16, 16, ktype, shared=shared)
+    live = c["pos"] >= 0
+    twice = np.flatnonzero(live[:-1] & (c["pos"][:-1] > 2))[::7]
+    for t in twice:                                     # the next token becomes a draft's second: rows t and t + 1 of one sequence
+        c["seq"][t + 1] = c["seq"][t]
+        c["pos"][t + 1] = c["pos"][t]
+        c["pos"][t] -= 1
+    out, lse = attend(c)
+    check(c, out, lse)
+    out, lse = attend(c, max_len=c["table"].shape[1] * 16)
+    check(c, out, lse)
+
+
+@pytest.mark.parametrize("G,ktype,dh", [(1, "f16", 64), (4, "f16", 128), (1, "f32", 64), (6, "f32", 128), (12, "f16", 80)])
+def test_attention_drafts_do_not_see_later_ones(G, ktype, dh):
+    """Several tokens of one sequence next to each other; the rows of the later ones hold NaN and infinities for the
+    earlier ones' sums to keep out, at every place in a step of rows."""
+    rng = np.random.default_rng(G)
+    for n in (4, 31, 33, 64, 66, 130):
+        for tokens in (2, 5, 9):
+            c = make(rng, [n + tokens, 20 + tokens], 2, G, dh, 16, ktype, tokens=tokens)
+            for bad in (math.nan, math.inf):
+                # the first sequence's last row: its last token alone attends it
+                p = n + tokens - 1
+                g, r = int(c["table"][0, p // 16]), p % 16
+                c["K"][g, :, r], c["V"][g, :, r] = bad, bad
+                out, lse = attend(c)
+                assert not out[tokens - 1].isfinite().any()
+                rest = [t for t in range(2 * tokens) if t != tokens - 1]
+                d = dict(c, q=c["q"][rest], pos=c["pos"][rest], seq=c["seq"][rest])
+                check(d, out[rest], lse[rest])
+
+
+def test_attention_groups_of_any_positions():
+    """Neighbouring tokens of one sequence with rising, falling, equal, idle and far positions, and bounds of the rows
+    that cut some of them off."""
+    rng = np.random.default_rng(16)
+    for G, ktype in ((1, "f16"), (4, "f16"), (2, "f32")):
+        c = make(rng, [400, 90], 2, G, 64, 16, ktype, tokens=16)
+        c["pos"][:16] = [3, 4, 5, 5, 399, 398, 0, 1, 2, 70, 140, 141, -1, 142, 399, 399]
+        c["pos"][16:] = [20, -1, -1, 21, 22, 23, 89, 88, 0, 0, 63, 64, 65, 66, -1, 89]
+        out, lse = attend(c)
+        check(c, out, lse)
+        d = dict(c, pos=np.minimum(c["pos"], 63))
+        out, lse = attend(c, max_len=64)               # rows from the bound on are not attended
+        check(d, out, lse)
+
+
 def test_attention_same_pages_and_tokens_twice():
     """Two slots of one sequence, a page twice in one row, the same head twice in a set: each is computed."""
     rng = np.random.default_rng(11)
