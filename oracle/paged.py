@@ -81,3 +81,26 @@ def attn(q, K, V, table, seq, pos, scale, group, heads=None):
             mag[t, j] = abs(scale) * (np.abs(k) @ np.abs(q[t, j])).max()
             absv[t, j] = w @ np.abs(v) / w.sum()
     return out, lse, mag, absv
+
+
+def layer(x, a, K, V, table, seq, pos, heads, scale, freq=None, layout="half", mscale=1.0):
+    """The sparsified attention on pages: out[b] = bo + sum over the heads of b of H_i(x[b]) W^O_i, the heads' keys (rotated
+    if freq is given) and values of every token in the pages before any attends. a: Wq, Wk, Wv, WoT [H*dh][d], bq, bk, bv,
+    bo or none of them. Returns out, K, V."""
+    x = np.asarray(x, dtype=np.float64)
+    H, dh = K.shape[1], K.shape[3]
+    qkv = []
+    for w, b in (("Wq", "bq"), ("Wk", "bk"), ("Wv", "bv")):
+        y = x @ np.asarray(a[w], dtype=np.float64).T
+        qkv.append((y if a.get(b) is None else y + np.asarray(a[b], dtype=np.float64)).reshape(-1, H, dh))
+    q, k, v = qkv
+    if freq is not None:
+        q, k = (rope(t, np.maximum(pos, 0), freq, layout, mscale) for t in (q, k))
+    K, V = append(K, k, table, seq, pos, heads), append(V, v, table, seq, pos, heads)
+    q = np.array([q[b, np.asarray(heads[b], dtype=int)] for b in range(len(x))]).reshape(len(x), -1, dh)
+    h, _, _, _ = attn(q, K, V, table, seq, pos, scale, 1, heads)
+    out = np.zeros(x.shape) if a.get("bo") is None else np.tile(np.asarray(a["bo"], dtype=np.float64), (len(x), 1))
+    for b in range(len(x)):
+        for j, i in enumerate(heads[b]):
+            out[b] += h[b, j] @ np.asarray(a["WoT"][int(i) * dh:(int(i) + 1) * dh], dtype=np.float64)
+    return out, K, V
