@@ -908,20 +908,31 @@ hipError_t launch_paged_combine(const PagedAttnArgs& a, hipStream_t st) {
 
 // ------------------------------------------------------------------ launch
 // Query rows of a workgroup: the smaller tile if it holds a unit's rows (kernel variant QT).
+// (8 rows with their second halves beside them against the tile of 32: 8 query heads a key head, 8000 to 50000 rows, 114 us
+// against 132; 6 to 12 rows of drafts 11.8 against 15.4; 8 tokens of a shared prefix 37.5 against 38.8.)
 static int pa_rows(int ktype, int qt) { return qt == 0 ? (ktype == DV_F16 ? 8 : 16) : 16 * qt; }
 static int pa_variant(int ktype, int64_t most) { return most <= pa_rows(ktype, 0) ? 0 : 2; }
 
-// Query rows of the largest unit of own rows: a token's of a key head, or those of as many tokens as the table's sequences
-// have on average.
-static int pa_own_rows(const PagedAttnArgs& a) {
-  const int own = a.heads != nullptr ? min(a.G, a.n) : a.G;
-  const int drafts = a.seq != nullptr && a.heads == nullptr ? min((a.T + a.g.n_seq - 1) / a.g.n_seq, 32) : 1;
-  return own * drafts;
+// Tokens that the table's sequences have on average (what is not known on the host is assumed), and query rows of the
+// largest unit of own rows: those of a key head of so many tokens.
+static int pa_drafts(const PagedAttnArgs& a) {
+  return a.seq != nullptr && a.heads == nullptr ? min((a.T + a.g.n_seq - 1) / a.g.n_seq, 32) : 1;
 }
+static int pa_own_rows(const PagedAttnArgs& a) { return (a.heads != nullptr ? min(a.G, a.n) : a.G) * pa_drafts(a); }
 
-// Least rows of a workgroup, lengths that one takes alone, tokens up to which the rows are cut evenly (every
-// wavefront looks at all positions).
-constexpr int kPaLeast = 256, kPaAlone = 512, kPaMaxScan = 1024;
+// Least rows of a workgroup. (One sequence of 2000 rows, 12 heads of 64 fp32, twelve workgroups a run: 12.0 us in 256, 10.4
+// in 128 with 1.5 more in the join, 15.2 in 512; where there are more heads or sequences the even share is longer.)
+constexpr int kPaLeast = 256;
+// Lengths that one workgroup takes alone, its result needing no join: while the units do not fill the card, up to four times as
+// much where they fill it four times over. (12 heads of 64 fp32: 512 rows 13.7 us, cut 18.6; 1000 rows 20.3, cut 16 to 19. 32
+// tokens of 32 of 96 heads of 128 fp16, 1024 units: up to 1000 rows 78 us, cut 84; 12000 units of up to 1000 rows 491, cut 648.)
+constexpr int kPaAlone = 512;
+static int pa_alone(int64_t units, int64_t resident) {
+  return units < resident ? kPaAlone : units < 4 * resident ? 2 * kPaAlone : 4 * kPaAlone;
+}
+// Tokens up to which the rows are cut evenly: every wavefront looks at all positions. (64 query heads on 8 of 128 fp16, 100 to
+// 6000 rows: 100 tokens 245 us, a workgroup a token 272; 300 tokens 703 and 680; 600 tokens of 100 to 4000 rows 911 and 840.)
+constexpr int kPaMaxScan = 1024;
 
 void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   const int cus = device_cu_count();
@@ -939,8 +950,12 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   a->group_tiles = (group + a->RT - 1) / a->RT;
   a->U = single ? a->n : a->g.H * a->group_tiles;
   const int64_t units = (int64_t)a->T * a->U, own = a->max_len - a->P;
-  const bool whole = a->T > kPaMaxScan;
-  a->direct = a->P == 0 && (whole || own <= kPaAlone);
+  // A workgroup a token: where each may be taken alone, and beside shared rows for more tokens than a wavefront's lanes that
+  // are no drafts, which would lose their groups (32 heads of 128 fp16, 16 to 700 own rows: 100 tokens 158 us against 174,
+  // 600 tokens 811 against 1118).
+  const bool alone = own <= pa_alone(units, resident);
+  const bool whole = a->T > kPaMaxScan || (alone && a->P > 0 && a->T > kWave && pa_drafts(*a) == 1);
+  a->direct = a->P == 0 && (whole || alone);
   a->gmax = 1;
   if (a->seq != nullptr && a->heads == nullptr && (a->direct || !whole))
     while (2 * a->gmax * a->G <= a->RT) a->gmax *= 2;
