@@ -429,12 +429,13 @@ class Rotary:
     _kept = _ck = None
 
     def c(self) -> CRotary:
-        # checked and built once per tensor (calls are on the hot path)
-        key = (self.layout, self.mscale)
-        if self.freq is not self._kept or self._ck != key:
-            _tensor("Rotary.freq", self.freq, (torch.float64,), 1)
-            self._cs = CRotary(2 * self.freq.shape[0], int(self.layout), _ptr(self.freq), float(self.mscale), 0)
-            self._ck, self._kept = key, self.freq
+        # checked and built once per tensor and memory of it (calls are on the hot path)
+        f = self.freq
+        key = (f.data_ptr(), f.shape, self.layout, self.mscale) if type(f) is torch.Tensor else None
+        if f is not self._kept or self._ck != key:
+            _tensor("Rotary.freq", f, (torch.float64,), 1)
+            self._cs = CRotary(2 * f.shape[0], int(self.layout), _ptr(f), float(self.mscale), 0)
+            self._ck, self._kept = key, f
         return self._cs
 
 
@@ -445,12 +446,16 @@ class PagedKV:
 
     def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor):
         self.K, self.V, self.table = K, V, table
-        self._kept = (None, None, None)
+        self._kept, self._ck = (None, None, None), None
+
+    def _key(self):
+        K, V, table = self.K, self.V, self.table
+        return K.data_ptr(), V.data_ptr(), table.data_ptr(), K.shape, V.shape, table.shape, K.stride(), V.stride()
 
     def c(self) -> CPagedKV:
-        # checked and built once per set of tensors (calls are on the hot path)
+        # checked and built once per set of tensors and memory of them (calls are on the hot path)
         kept = self._kept
-        if self.K is not kept[0] or self.V is not kept[1] or self.table is not kept[2]:
+        if self.K is not kept[0] or self.V is not kept[1] or self.table is not kept[2] or self._ck != self._key():
             for nm in ("K", "V"):
                 t = getattr(self, nm)
                 if not isinstance(t, torch.Tensor):
@@ -469,9 +474,11 @@ class PagedKV:
                 raise ValueError("PagedKV: K and V must have the same shape and strides")
             _tensor("PagedKV.table", self.table, _I32, 2, dev=False)
             _gpu("PagedKV", self.K, self.V, self.table)
+            if not self.K.device == self.V.device == self.table.device:
+                raise ValueError("PagedKV: K, V and the table must be on one device")
             self._cs = CPagedKV(H, dh, page, n_pages, self.table.shape[0], self.table.shape[1], _wtype(self.K), 0,
                                 *strides, _ptr(self.K), _ptr(self.V), _ptr(self.table))
-            self._kept = (self.K, self.V, self.table)
+            self._kept, self._ck = (self.K, self.V, self.table), self._key()
         return self._cs
 
 
