@@ -241,7 +241,7 @@ static hipError_t launch_rope_t(RopeArgs a, hipStream_t st) {
   const int gx = (int)(blocks < kRopeGridX ? blocks : kRopeGridX);
   const dim3 grid(gx, (int)((blocks + gx - 1) / gx));
   if constexpr (E > 1) {
-    if ((double)a.T * a.per * E * sizeof(KT) > kL2Bytes) {
+    if ((double)a.T * (a.nq + (a.append ? 2 * a.nk : 0)) * a.dh * sizeof(KT) > kL2Bytes) {
       launch_k((k_rope<IT, KT, E, HALF, true>), grid, dim3(kRopeNT), 0, st, a);
       return hipGetLastError();
     }

@@ -81,6 +81,54 @@ def test_rope(T, H, dh, rot, layout, dtype, inverse):
     assert torch.equal(out, x)
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("xtype,ktype", [("f16", "f16"), ("f32", "f16"), ("f16", "f32")])
+def test_large_results(layout, xtype, ktype):
+    """More than L2 holds (stored past it): a rotation in place and an append, every element."""
+    rng = np.random.default_rng(20)
+    T, Hq, H, dh, rot, page = 600, 230, 70, 128, 96, 32
+    freq = P.freqs(rot)
+    r = B.Rotary(dev(freq), LAYOUT[layout])
+    table = rng.permutation(2 * 12).astype(np.int32).reshape(2, 12)
+    pos = np.concatenate([np.arange(250), np.arange(3, 353)]).astype(np.int32)
+    seq = np.repeat(np.array([0, 1], dtype=np.int32), [250, 350])
+    q, k, v = (torch.randn(T, n, dh, dtype=DT[xtype], device="cuda") for n in (Hq, H, H))
+    K, V = (torch.full((24, H, page, dh), 5.0, dtype=DT[ktype], device="cuda") for _ in range(2))
+    want = P.rope(h64(q), pos, freq, layout)
+    bound = rope_bound(h64(q), freq, layout, 1.0, want, xtype)
+    qo = B.dv_paged_append(B.PagedKV(K, V, dev(table)), k, v, dev(pos), seq=dev(seq), rotary=r, q=q)
+    assert (np.abs(h64(qo) - want) <= bound).all()
+    B.dv_rope(r, q, dev(pos), out=q)
+    assert torch.equal(q, qo)
+    kr = P.rope(h64(k), pos, freq, layout)
+    g, row = table[seq, pos // page], pos % page
+    assert (np.abs(h64(K)[g, :, row] - kr) <= rope_bound(h64(k), freq, layout, 1.0, kr, ktype)).all()
+    assert torch.equal(V[torch.from_numpy(g).long().cuda(), :, torch.from_numpy(row).long().cuda()], v.to(DT[ktype]))
+    mask = torch.ones(24, page, dtype=torch.bool, device="cuda")
+    mask[torch.from_numpy(g).long().cuda(), torch.from_numpy(row).long().cuda()] = False
+    assert (K.transpose(1, 2)[mask] == 5.0).all() and (V.transpose(1, 2)[mask] == 5.0).all()
+
+
+def test_descriptors_follow_their_tensors():
+    """New memory or another shape under the tensors of a PagedKV or Rotary is what the next call uses."""
+    table = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    K, V = (torch.zeros(1, 1, 4, 8, dtype=torch.float32, device="cuda") for _ in range(2))
+    freq = torch.ones(2, dtype=torch.float64, device="cuda")
+    kv, rot = B.PagedKV(K, V, table), B.Rotary(freq)
+    k = torch.ones(1, 1, 8, device="cuda")
+    pos = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.dv_paged_append(kv, k, k, pos, rotary=rot)
+    old = K.detach()
+    K.data = torch.zeros(1, 1, 2, 8, dtype=torch.float32, device="cuda")
+    with pytest.raises(ValueError):
+        B.dv_paged_append(kv, k, k, pos, rotary=rot)   # V has the other shape still
+    V.data = torch.zeros(1, 1, 2, 8, dtype=torch.float32, device="cuda")
+    freq.data = torch.zeros(4, dtype=torch.float64, device="cuda")
+    B.dv_paged_append(kv, 3 * k, 3 * k, pos + 1, rotary=rot)
+    assert (K[0, 0, 1] == 3.0).all() and (K[0, 0, 0] == 0.0).all() and (V[0, 0, 1] == 3.0).all()
+    assert (old[0, 0, 0] == 1.0).all() and (old[0, 0, 1] == 0.0).all()
+
+
 def test_rope_strided_unaligned_and_empty():
     """A slice of a fused projection, an odd element offset (the narrow path), no tokens; what lies between tokens
     is left as it was."""
