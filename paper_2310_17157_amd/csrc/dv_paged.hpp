@@ -61,7 +61,8 @@ struct PagedAttnArgs {
   int P, SP, CP;                    // shared rows, parts of them, rows of a part
   int n_shared;                     // workgroups of the shared rows
   int target;                       // workgroups that the own rows are cut for (0: an item is a token)
-  int items, cmin;                  // items at most, least rows of one
+  int items, cmin, cstep;           // items at most, least rows of one, what its rows are a multiple of
+  int live;                         // units of a token that have query rows, at most
   int gmax, RW;                     // tokens of a group at most, rows that a workgroup keeps partials of
   bool direct;                      // one part each: written out by the attention itself
   float *sml, *so, *oml, *oo;       // partials of shared and own rows

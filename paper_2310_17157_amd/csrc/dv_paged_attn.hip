@@ -123,13 +123,13 @@ __device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, const PaTok& fir
     rows += (float)pa_last(pa_wave_incl((n + 63) >> 6)) * 64.f;
     most = max(most, pa_wave_max(n));
   }
-  const float even = fminf(rows * (float)a.U / (float)a.target + 1.f, 1e9f);
+  const float even = fminf(rows * (float)a.live / (float)a.target + 1.f, 1e9f);
   PaCut c;
   int chunk = max(max(a.cmin, (int)even), most / (kPaMaxParts - 1) + 1);
   // An even share gives every group a rest beside it: where the card could hold all groups at once, a quarter more rows
   // at a time until it holds all runs and rests, which then need no second round.
   for (int k = 0; k < 8; ++k) {
-    c.chunk = (chunk + 127) & ~127;
+    c.chunk = (chunk + a.cstep - 1) & -a.cstep;
     c.inv = 1.f / (float)c.chunk;
     c.whole = 0;
     int rests = 0, groups = 0;
@@ -139,7 +139,7 @@ __device__ __forceinline__ PaCut pa_cut(const PagedAttnArgs& a, const PaTok& fir
       rests += __popcll(__ballot(n - w * c.chunk > 0));
       groups += __popcll(__ballot(n > 0));
     }
-    if ((int64_t)(c.whole + rests) * a.U <= a.target || (int64_t)groups * a.U > a.target) break;
+    if ((int64_t)(c.whole + rests) * a.live <= a.target || (int64_t)groups * a.live > a.target) break;
     chunk = c.chunk + (c.chunk >> 2);
   }
   return c;
@@ -920,15 +920,19 @@ static int pa_drafts(const PagedAttnArgs& a) {
 }
 static int pa_own_rows(const PagedAttnArgs& a) { return (a.heads != nullptr ? min(a.G, a.n) : a.G) * pa_drafts(a); }
 
-// Least rows of a workgroup. (One sequence of 2000 rows, 12 heads of 64 fp32, twelve workgroups a run: 12.0 us in 256, 10.4
-// in 128 with 1.5 more in the join, 15.2 in 512; where there are more heads or sequences the even share is longer.)
-constexpr int kPaLeast = 256;
-// Lengths that one workgroup takes alone, its result needing no join: while the units do not fill the card, up to four times as
-// much where they fill it four times over. (12 heads of 64 fp32: 512 rows 13.7 us, cut 18.6; 1000 rows 20.3, cut 16 to 19. 32
+// Least rows of a workgroup: 64 KB of keys, 64 to 256 of them. (One sequence of 2000 rows, 12 heads of 64 fp32, twelve workgroups
+// a run: 12.0 us in 256, 10.4 in 128 with 1.5 more in the join, 15.2 in 512; where there are more heads or sequences
+// the even share is longer. 2 tokens, 8 query on 2 heads of 256 fp32, 372 and 1206 rows: 26.7 us in 256, 21.9 in 64.
+// 24 drafts of 5 heads of 192 fp32 on 1184 shared rows: 58 and 35.)
+constexpr int kPaLeastBytes = 65536;
+static int pa_least(const PagedAttnArgs& a, int ktype) {
+  return min(max(kPaLeastBytes / (a.g.dh * (ktype == DV_F16 ? 2 : 4)), 64), 256);
+}
+// Lengths that one workgroup takes alone, its result needing no join: twice the least while the units do not fill the card,
+// up to eight times it where they fill it four times over. (12 heads of 64 fp32: 512 rows 13.7 us, cut 18.6; 1000 rows 20.3, cut 16 to 19. 32
 // tokens of 32 of 96 heads of 128 fp16, 1024 units: up to 1000 rows 78 us, cut 84; 12000 units of up to 1000 rows 491, cut 648.)
-constexpr int kPaAlone = 512;
-static int pa_alone(int64_t units, int64_t resident) {
-  return units < resident ? kPaAlone : units < 4 * resident ? 2 * kPaAlone : 4 * kPaAlone;
+static int pa_alone(int least, int64_t units, int64_t resident) {
+  return (units < resident ? 2 : units < 4 * resident ? 4 : 8) * least;
 }
 // Tokens up to which the rows are cut evenly: every wavefront looks at all positions. (64 query heads on 8 of 128 fp16, 100 to
 // 6000 rows: 100 tokens 245 us, a workgroup a token 272; 300 tokens 703 and 680; 600 tokens of 100 to 4000 rows 911 and 840.)
@@ -949,11 +953,16 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
   a->row_tiles = a->P > 0 ? (int)(((int64_t)a->T * group + a->RTS - 1) / a->RTS) : 0;
   a->group_tiles = (group + a->RT - 1) / a->RT;
   a->U = single ? a->n : a->g.H * a->group_tiles;
-  const int64_t units = (int64_t)a->T * a->U, own = a->max_len - a->P;
+  // units of a token that have query rows: of a set of grouped heads as many as it has heads at most (64 tokens of 1 of 8 heads
+  // on 4, 4000 to 17600 rows: 103 us, cut as if all four had some 183)
+  a->live = a->heads != nullptr ? min(a->U, a->n) : a->U;
+  a->cmin = pa_least(*a, ktype);
+  a->cstep = kPaNW * (ktype == DV_F16 ? 32 : 16);
+  const int64_t units = (int64_t)a->T * a->live, own = a->max_len - a->P;
   // A workgroup a token: where each may be taken alone, and beside shared rows for more tokens than a wavefront's lanes that
   // are no drafts, which would lose their groups (32 heads of 128 fp16, 16 to 700 own rows: 100 tokens 158 us against 174,
   // 600 tokens 811 against 1118).
-  const bool alone = own <= pa_alone(units, resident);
+  const bool alone = own <= pa_alone(a->cmin, units, resident);
   const bool whole = a->T > kPaMaxScan || (alone && a->P > 0 && a->T > kWave && pa_drafts(*a) == 1);
   a->direct = a->P == 0 && (whole || alone);
   a->gmax = 1;
@@ -961,7 +970,7 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
     while (2 * a->gmax * a->G <= a->RT) a->gmax *= 2;
   a->RW = min(a->RT, a->gmax * group);
   // The shared rows' parts: their share of the resident workgroups if all tokens had max_len (but no more than as many rows
-  // of their own), one a CU at least, kPaLeast rows each at least.
+  // of their own), one a CU at least, the least rows each at least.
   a->SP = 0;
   a->CP = 1;
   int64_t shared = 0;
@@ -969,15 +978,14 @@ void plan_paged_attn(PagedAttnArgs* a, int ktype) {
     const int64_t tiles = (int64_t)a->g.H * a->row_tiles;
     const int64_t cost = tiles * a->P, others = units * min(own, (int64_t)a->P);
     const int64_t want = max((int64_t)cus, resident * cost / (cost + others));
-    const int64_t parts = max((int64_t)1, min(min((int64_t)kPaMaxParts, (want + tiles - 1) / tiles), (int64_t)a->P / kPaLeast));
-    a->CP = (int)((a->P + parts - 1) / parts + 127) / 128 * 128;
+    const int64_t parts = max((int64_t)1, min(min((int64_t)kPaMaxParts, (want + tiles - 1) / tiles), (int64_t)a->P / a->cmin));
+    a->CP = (int)((a->P + parts - 1) / parts + a->cstep - 1) / a->cstep * a->cstep;
     a->SP = (a->P + a->CP - 1) / a->CP;
     shared = tiles * a->SP;
   }
   a->n_shared = a->P > 0 ? (a->g.H * a->SP + 7) / 8 * 8 * a->row_tiles : 0;
-  a->cmin = kPaLeast;
   a->target = a->direct || whole ? 0 : (int)max(resident - shared, (int64_t)cus);
-  a->items = a->T + (a->target > 0 ? (a->target + a->U - 1) / a->U : 0);
+  a->items = a->T + (a->target > 0 ? (a->target + a->live - 1) / a->live : 0);
 }
 
 template <typename KT, int DH, int QS, int QO, bool FULL>
